@@ -50,20 +50,22 @@ typedef enum {
     SMOE_ENOMEM = -4    /* host allocation for the handle failed                         */
 } smoe_status;
 
-enum { SMOE_F32 = 0, SMOE_BF16 = 1 };
+enum { SMOE_F32 = 0, SMOE_BF16 = 1, SMOE_MXFP8 = 2 };
 enum { SMOE_GATE_FULL = 0, SMOE_GATE_RENORM = 1 };
 
 typedef struct smoe_layer smoe_layer_t;
 
 /* Layer shape.  E experts in the full bank, K resident slots (1 <= K <= E),
  * d_model -> d_ff -> ReLU -> d_model experts without biases.  dtype is the
- * storage type of activations AND expert weights (SMOE_F32 or SMOE_BF16).
+ * storage type of activations AND expert weights (SMOE_F32 or SMOE_BF16); with
+ * SMOE_MXFP8 activations and bank are bf16 and the resident slots 8-bit (see
+ * smoe_expert_ffn_mx).
  * gate_mode: SMOE_GATE_FULL  gate = softmax over all E, read at the served expert;
  *            SMOE_GATE_RENORM the same divided by the resident experts' total.
  * spare_slots: physical weight slots beyond K that smoe_update_tick loads into while the
  *            K mapped ones keep serving (see the asynchronous update calls below).
- * Limits: E <= 256; K <= E; for SMOE_BF16, d_model and d_ff must be
- * multiples of 32 (the MFMA fragment width); max_tokens >= 1. */
+ * Limits: E <= 256; K <= E; for SMOE_BF16 and SMOE_MXFP8, d_model and d_ff must
+ * be multiples of 32 (the MFMA fragment width); max_tokens >= 1. */
 typedef struct {
     int32_t E, K, d_model, d_ff, max_tokens;
     int32_t dtype;
@@ -88,8 +90,9 @@ size_t smoe_workspace_bytes(const smoe_layer_t* layer);
  * SMOE_BF16 the library keeps each slot in a tiled order that feeds the matrix
  * cores with contiguous loads (see smoe_set_resident), so they can only be
  * filled through smoe_set_resident / smoe_update_tick.
- * Equals (K + spare_slots) * d_model * d_ff * sizeof(dtype): always size the
- * arrays with this call, never with K alone. */
+ * Equals (K + spare_slots) * d_model * d_ff * sizeof(dtype) for SMOE_F32 and
+ * SMOE_BF16, about 33/64 of the bf16 figure for SMOE_MXFP8: always size the arrays
+ * with this call, never with K alone. */
 size_t smoe_slot_weight_bytes(const smoe_layer_t* layer);
 
 /* Binds the caller-owned device buffers the layer works on.
@@ -306,6 +309,97 @@ int smoe_update_pending(const smoe_layer_t* layer);
  * computed in fp32 and rounded once to the layer's dtype. */
 int smoe_combine(smoe_layer_t* layer, const void* y_perm, const int32_t* inv_perm, const float* gate,
                  const void* residual, int T, void* out, void* stream);
+
+/* ---- Layers that serve k experts per token --------------------------------
+ * The steps of smoe_route .. smoe_combine for k > 1, the norm in front of them,
+ * and expert products on 8-bit values.  A batch of T tokens has T * k (token,
+ * choice) pairs, token * k + choice, each an entry of the per-token arrays:
+ * every call needs T * k <= max_tokens, k <= 16, and smoe_importance and
+ * smoe_expert_ffn take the pairs as T * k tokens.
+ *
+ * 8-bit rows: e4m3 values in blocks of 32 consecutive elements, each block with
+ * one power of two 2^e, the smallest with which no magnitude of the block
+ * exceeds 448 (e kept to [-126, 127]).  q [T, d_model] holds the values in units of their block's
+ * scale; q_scale [T, smoe_mx_scale_pitch(d_model)] holds e + 127 per block, one
+ * byte each, rows filled up to a multiple of 8 bytes. */
+
+/* Bytes of one row of q_scale: d_model / 32 rounded up to a multiple of 8 (0
+ * where d_model is not a positive multiple of 32). */
+size_t smoe_mx_scale_pitch(int d_model);
+
+/* Residual addition and root-mean-square norm, for each of T rows:
+ *   h = x + residual (residual may be NULL);  total = h
+ *   y = h / sqrt(mean(h^2) + eps) * weight;  q, q_scale = y as 8-bit rows
+ * computed in fp32 from the unrounded sum; total and y are rounded once to the
+ * layer's activation type.  weight [d_model] fp32, 16-byte aligned.  Any of
+ * total, y and the pair (q, q_scale) may be NULL, not all; 8-bit rows need
+ * d_model % 32 == 0, and their bytes behind the last block of a row of q_scale
+ * become 0.  total and y may alias x or residual, but not each other.  Uses the
+ * handle's shape only: it need not be bound. */
+int smoe_add_norm(smoe_layer_t* layer, const void* x, const void* residual, const float* weight, float eps,
+                  int T, void* total, void* y, void* q, void* q_scale, void* stream);
+
+/* How k experts are chosen for a token from its logits l:
+ *   score   s = softmax(l) over all E (SMOE_SCORE_SOFTMAX) or sigmoid(l)
+ *   choice  by s + bias: the E experts are `groups` equal groups of consecutive
+ *           ids; a group ranks by the sum of its group_best (1 or 2) largest values,
+ *           the groups_kept best groups stay, and among their experts the k
+ *           largest values are chosen, best first (lower id, lower group on a tie)
+ *   weight  s, without the bias; divided by the sum over the chosen experts with
+ *           renorm = 1; times scale
+ * Limits: k <= 16, groups <= 16 and a divisor of E, k <= the experts of
+ * groups_kept groups. */
+enum { SMOE_SCORE_SOFTMAX = 0, SMOE_SCORE_SIGMOID = 1 };
+typedef struct {
+    int32_t k, score, groups, groups_kept, group_best, renorm;
+    float scale;
+} smoe_topk_rule;
+
+/* Router and Masked Gating for k experts per token.  x [T, d_model], bias [E]
+ * fp32 or NULL.  For every token, with choices in order:
+ *   orig_expert, orig_gate [T, k]  the rule applied to all experts
+ *   slot, gate [T, k]              the rule applied to the resident experts alone: a
+ *       group of which none is resident is not kept, one with a single resident
+ *       expert ranks by that one; where fewer than k can be had, the rest is
+ *       slot -1, gate 0 (softmax still runs over all E, renorm over the served)
+ *   xnorm [T, k]                   |x_t|, k times
+ * so that smoe_importance takes the T * k pairs as they are.  The layer's
+ * gate_mode plays no part.  Choices nearer to one another than the error of an
+ * fp32 logit are decided again in 64 bits.  The first call after a bind
+ * prepares the router's weights in the workspace; router_w must still hold them at
+ * later calls.  SMOE_ESTATE until every slot has been filled. */
+int smoe_route_topk(smoe_layer_t* layer, const smoe_topk_rule* rule /*host*/, const float* bias, const void* x,
+                    int T, int32_t* orig_expert, float* orig_gate, int32_t* slot, float* gate, float* xnorm,
+                    void* stream);
+
+/* Stable counting sort of the T * k pairs by slot [T, k]; a value outside [0,K)
+ * is a pair that nobody serves.  perm [T * k] (position -> pair), inv_perm [T, k]
+ * (pair -> position, -1 if not served), offsets [K+1] as in smoe_permute;
+ * x_perm[pos, :] = x[perm[pos] / k, :].  x_perm may be NULL (then x too):
+ * only the indexes are written, which is all that smoe_expert_ffn_mx needs.  Positions
+ * from offsets[K] on are left as they were in perm and x_perm. */
+int smoe_permute_topk(smoe_layer_t* layer, const void* x, const int32_t* slot, int T, int k, void* x_perm,
+                      int32_t* perm, int32_t* inv_perm, int32_t* offsets, void* stream);
+
+/* Grouped expert FFN on 8-bit values (SMOE_MXFP8 layers): sorted row r, with
+ * offsets[k] <= r < offsets[k+1], belongs to slot k and token perm[r] / k, or
+ * token r where perm is NULL (k = 1), and gets
+ *   y_perm[r, :] = h W2_k,  h = ReLU(x W1_k)
+ * x being the token's 8-bit row of q [T, d_model] and q_scale, W1_k and W2_k the
+ * slot's matrices, which smoe_set_resident and smoe_update_tick round from the bf16
+ * bank to blocks of 32 consecutive elements of a column (along the reduction), and h rounded
+ * to blocks of 32 features between the products; products and sums on the
+ * matrix cores in fp32, y_perm bf16, rounded once.  Rows from offsets[K] on are
+ * left as they were. */
+int smoe_expert_ffn_mx(smoe_layer_t* layer, const void* q, const void* q_scale, const int32_t* perm, int k,
+                       const int32_t* offsets, int T, void* y_perm, void* stream);
+
+/* Weighted sum of a token's k results, in token order:
+ *   out[t, :] = sum_j gate[t, j] * y_perm[inv_perm[t, j], :]  (+ residual[t, :] if not NULL)
+ * in fp32, choices in their order, rounded once to the layer's activation type;
+ * a choice with inv_perm -1 adds nothing.  residual may alias out. */
+int smoe_combine_topk(smoe_layer_t* layer, const void* y_perm, const int32_t* inv_perm, const float* gate,
+                      const void* residual, int T, int k, void* out, void* stream);
 
 #ifdef __cplusplus
 }

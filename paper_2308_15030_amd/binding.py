@@ -19,9 +19,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SMOE_LIBRARY") or os.path.join(_HERE, "libswapmoe.so")
 
 SMOE_OK, SMOE_EINVAL, SMOE_ESTATE, SMOE_EHIP, SMOE_ENOMEM = 0, -1, -2, -3, -4
-SMOE_F32, SMOE_BF16 = 0, 1
+SMOE_F32, SMOE_BF16, SMOE_MXFP8 = 0, 1, 2
 SMOE_GATE_FULL, SMOE_GATE_RENORM = 0, 1
 SMOE_POLICY_IMPORTANCE, SMOE_POLICY_COUNT, SMOE_POLICY_MAGNITUDE = 0, 1, 2
+SMOE_SCORE_SOFTMAX, SMOE_SCORE_SIGMOID = 0, 1
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -35,6 +36,13 @@ class smoe_config(C.Structure):
     _fields_ = [("E", C.c_int32), ("K", C.c_int32), ("d_model", C.c_int32), ("d_ff", C.c_int32),
                 ("max_tokens", C.c_int32), ("dtype", C.c_int32), ("gate_mode", C.c_int32),
                 ("spare_slots", C.c_int32)]
+
+
+class smoe_topk_rule(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("k", "score", "groups", "groups_kept", "group_best", "renorm")] + [("scale", C.c_float)]
+
+    def __init__(self, k, score=SMOE_SCORE_SOFTMAX, groups=1, groups_kept=1, group_best=1, renorm=1, scale=1.0):
+        super().__init__(k, score, groups, groups_kept, group_best, renorm, scale)
 
 
 _vp, _i = C.c_void_p, C.c_int
@@ -69,6 +77,12 @@ _SIGS = {
     "smoe_update_on_device": (C.c_int, [_vp, _vp, _vp, _vp, _vp]),
     "smoe_profile_stream_read": (C.c_int, [_vp, _i, _vp]),
     "smoe_forward": (C.c_int, [_vp, _vp, _i, _vp, _vp, _i] + [_vp] * 12),
+    "smoe_mx_scale_pitch": (C.c_size_t, [_i]),
+    "smoe_add_norm": (C.c_int, [_vp, _vp, _vp, _vp, C.c_float, _i] + [_vp] * 5),
+    "smoe_route_topk": (C.c_int, [_vp, C.POINTER(smoe_topk_rule), _vp, _vp, _i] + [_vp] * 6),
+    "smoe_permute_topk": (C.c_int, [_vp, _vp, _vp, _i, _i] + [_vp] * 5),
+    "smoe_expert_ffn_mx": (C.c_int, [_vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp]),
+    "smoe_combine_topk": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 for _name, (_res, _args) in _SIGS.items():
@@ -190,6 +204,35 @@ def smoe_forward(layer, x, T, residual, out, accumulate, orig_expert, orig_gate,
     _check(_lib.smoe_forward(layer, _ptr(x), T, _ptr(residual), _ptr(out), int(accumulate), _ptr(orig_expert),
                              _ptr(orig_gate), _ptr(slot), _ptr(gate), _ptr(xnorm), _ptr(count), _ptr(gsum),
                              _ptr(score), _ptr(perm), _ptr(inv_perm), _ptr(offsets), _stream(stream)))
+
+
+def smoe_mx_scale_pitch(d_model) -> int:
+    return _lib.smoe_mx_scale_pitch(d_model)
+
+
+def smoe_add_norm(layer, x, residual, weight, eps, T, total, y, q, q_scale, stream=None):
+    _check(_lib.smoe_add_norm(layer, _ptr(x), _ptr(residual), _ptr(weight), eps, T, _ptr(total), _ptr(y), _ptr(q),
+                              _ptr(q_scale), _stream(stream)))
+
+
+def smoe_route_topk(layer, rule, bias, x, T, orig_expert, orig_gate, slot, gate, xnorm, stream=None):
+    _check(_lib.smoe_route_topk(layer, rule, _ptr(bias), _ptr(x), T, _ptr(orig_expert), _ptr(orig_gate), _ptr(slot),
+                                _ptr(gate), _ptr(xnorm), _stream(stream)))
+
+
+def smoe_permute_topk(layer, x, slot, T, k, x_perm, perm, inv_perm, offsets, stream=None):
+    _check(_lib.smoe_permute_topk(layer, _ptr(x), _ptr(slot), T, k, _ptr(x_perm), _ptr(perm), _ptr(inv_perm),
+                                  _ptr(offsets), _stream(stream)))
+
+
+def smoe_expert_ffn_mx(layer, q, q_scale, perm, k, offsets, T, y_perm, stream=None):
+    _check(_lib.smoe_expert_ffn_mx(layer, _ptr(q), _ptr(q_scale), _ptr(perm), k, _ptr(offsets), T, _ptr(y_perm),
+                                   _stream(stream)))
+
+
+def smoe_combine_topk(layer, y_perm, inv_perm, gate, residual, T, k, out, stream=None):
+    _check(_lib.smoe_combine_topk(layer, _ptr(y_perm), _ptr(inv_perm), _ptr(gate), _ptr(residual), T, k, _ptr(out),
+                                  _stream(stream)))
 
 
 def smoe_set_profile_events(layer, g1_begin, g1_end, g2_begin, g2_end):
@@ -424,3 +467,52 @@ class Layer:
         self.expert_ffn(T)
         self.combine(T, residual, out)
         return self.out if out is None else out
+
+    # layers that serve k experts per token: per-pair results in the same buffers, pair = token * k + choice
+    def mx_buffers(self, T):
+        """Buffers for T 8-bit rows: values [T, d_model] and scales [T, smoe_mx_scale_pitch(d_model)], uint8 both."""
+        return (torch.empty(T, self.d_model, dtype=torch.uint8, device=self.device),
+                torch.empty(T, smoe_mx_scale_pitch(self.d_model), dtype=torch.uint8, device=self.device))
+
+    def add_norm(self, x, T, weight, eps, residual=None, total=None, y=None, q=None, q_scale=None):
+        smoe_add_norm(self.handle, x, residual, weight, eps, T, total, y, q, q_scale)
+
+    def route_topk(self, x, T, rule, bias=None):
+        smoe_route_topk(self.handle, rule, bias, x, T, self.orig_expert, self.orig_gate, self.slot, self.gate, self.xnorm)
+
+    def permute_topk(self, x, T, k):
+        """x None: the indexes alone, for expert_ffn_mx."""
+        smoe_permute_topk(self.handle, x, self.slot, T, k, None if x is None else self.x_perm, self.perm, self.inv_perm,
+                          self.offsets)
+
+    def expert_ffn_mx(self, q, q_scale, T, k):
+        smoe_expert_ffn_mx(self.handle, q, q_scale, self.perm, k, self.offsets, T, self.y_perm)
+        return self.y_perm
+
+    def combine_topk(self, T, k, residual=None, out=None):
+        out = self.out if out is None else out
+        smoe_combine_topk(self.handle, self.y_perm, self.inv_perm, self.gate, residual, T, k, out)
+        return out
+
+    def forward_topk(self, x, T, rule, bias=None, accumulate=1, residual=None, out=None, q=None, q_scale=None):
+        """Route, importance, sort, expert FFN and weighted sum with rule.k experts per token.  Layers with 8-bit slots
+        take the rows of x in 8 bits too (q, q_scale of add_norm)."""
+        k = rule.k
+        self.route_topk(x, T, rule, bias)
+        self.importance(T * k, accumulate)
+        if self.dtype == SMOE_MXFP8:
+            self.permute_topk(None, T, k)
+            self.expert_ffn_mx(q, q_scale, T, k)
+        else:
+            self.permute_topk(x, T, k)
+            self.expert_ffn(T * k)
+        return self.combine_topk(T, k, residual, out)
+
+    def block_topk(self, x, T, weight, eps, rule, y, residual=None, total=None, bias=None, accumulate=1, out=None, q=None,
+                   q_scale=None):
+        """A whole pre-norm block: total = x + residual, y = norm(total) (in 8 bits too where q is given), the layer on y,
+        and total added to its result.  total None: x itself is the stream (then residual must be None)."""
+        if total is None and residual is not None:
+            raise ValueError("block_topk: the sum of x and residual needs a buffer (total)")
+        self.add_norm(x, T, weight, eps, residual, total, y, q, q_scale)
+        return self.forward_topk(y, T, rule, bias, accumulate, x if total is None else total, out, q, q_scale)

@@ -66,10 +66,11 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
     w.hist32 = off;  off = align_up(off + (size_t)((c.max_tokens + 31) / 32) * c.K * 4, 256);
     // hidden activations: every segment is re-based to a multiple of 32 rows
     const size_t rows = std::max((size_t)c.max_tokens + 32 * (size_t)c.K, smoe_small_batch_rows(c));
-    w.hidden = off;  off = align_up(off + rows * c.d_ff * smoe_elem_size(c.dtype), 256);
-    // bf16 path: the router's weights in matrix-operand order, experts padded to a multiple of 32
+    const size_t hidden = c.dtype == SMOE_MXFP8 ? smoe_mx_hidden_bytes(c) : rows * c.d_ff * smoe_elem_size(c.dtype);
+    w.hidden = off;  off = align_up(off + hidden, 256);
+    // bf16 activations: the router's weights in matrix-operand order, experts padded to a multiple of 32
     w.rsplit = off;
-    if (c.dtype == SMOE_BF16) off = align_up(off + (size_t)((c.E + 31) / 32 * 32) * c.d_model * 4, 256);
+    if (c.dtype != SMOE_F32) off = align_up(off + (size_t)((c.E + 31) / 32 * 32) * c.d_model * 4, 256);
     // ... and the partial logits of few tokens: 8 slices of 32 experts, or 4 of 64, 128 or 256; sums of squares behind them
     w.rpart = off;
     if (c.dtype == SMOE_BF16) {
@@ -77,6 +78,7 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
         off = align_up(off + SMOE_FEW_T * (logits + 8 * 2) * 4, 256);
     }
     w.norm = off;    off = align_up(off + (size_t)c.E * 64 * 4, 256);      // smoe_expert_norm partial sums
+    w.rnorm = off;   off += 256;                                           // smoe_route_topk: largest norm of a router row
     // asynchronous loads from a host bank land here (copy engine) before they are packed into a slot
     w.stage = off;   off = align_up(off + (size_t)c.spare_slots * 2 * c.d_model * c.d_ff * smoe_elem_size(c.dtype), 256);
     w.total = off;
@@ -90,7 +92,7 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
 constexpr int TRAFFIC_DEVICES = 64;
 static std::atomic<uint64_t> g_slot_traffic[TRAFFIC_DEVICES];
 static uint64_t layer_slot_bytes(const smoe_config& c) {
-    return 2ull * (c.K + c.spare_slots) * c.d_model * c.d_ff * smoe_elem_size(c.dtype);
+    return 2ull * (c.K + c.spare_slots) * smoe_slot_bytes(c);
 }
 
 static int traffic_device() {
@@ -110,7 +112,7 @@ static void note_slot_pass(smoe_layer* L) {
 
 // A slot of L changes hands: traffic for the other layers, L's own bytes are counted as such.
 static void note_slot_load(smoe_layer* L) {
-    const uint64_t one = 2ull * L->cfg.d_model * L->cfg.d_ff * smoe_elem_size(L->cfg.dtype);
+    const uint64_t one = 2ull * smoe_slot_bytes(L->cfg);
     const int dev = traffic_device();
     g_slot_traffic[dev].fetch_add(one, std::memory_order_relaxed);
     if (L->slot_device == dev) L->slot_traffic_seen += one;
@@ -159,14 +161,14 @@ int smoe_create(const smoe_config* cfg, smoe_layer_t** out) {
         return smoe_fail(SMOE_EINVAL, "smoe_create: d_model=%d d_ff=%d out of range", c.d_model, c.d_ff);
     if (c.max_tokens < 1 || c.max_tokens > (1 << 24))
         return smoe_fail(SMOE_EINVAL, "smoe_create: max_tokens=%d outside [1,2^24]", c.max_tokens);
-    if (c.dtype != SMOE_F32 && c.dtype != SMOE_BF16)
+    if (c.dtype != SMOE_F32 && c.dtype != SMOE_BF16 && c.dtype != SMOE_MXFP8)
         return smoe_fail(SMOE_EINVAL, "smoe_create: unknown dtype %d", c.dtype);
     if (c.gate_mode != SMOE_GATE_FULL && c.gate_mode != SMOE_GATE_RENORM)
         return smoe_fail(SMOE_EINVAL, "smoe_create: unknown gate_mode %d", c.gate_mode);
     if (c.spare_slots < 0 || c.spare_slots > 8)
         return smoe_fail(SMOE_EINVAL, "smoe_create: spare_slots=%d outside [0,8]", c.spare_slots);
-    if (c.dtype == SMOE_BF16 && (c.d_model % 32 || c.d_ff % 32))
-        return smoe_fail(SMOE_EINVAL, "smoe_create: bf16 needs d_model and d_ff to be multiples of 32");
+    if (c.dtype != SMOE_F32 && (c.d_model % 32 || c.d_ff % 32))
+        return smoe_fail(SMOE_EINVAL, "smoe_create: bf16 and 8-bit layers need d_model and d_ff to be multiples of 32");
     if (c.dtype == SMOE_F32 && (c.d_model % 4 || c.d_ff % 4))
         return smoe_fail(SMOE_EINVAL, "smoe_create: fp32 needs d_model and d_ff to be multiples of 4");
     smoe_layer* L = new (std::nothrow) smoe_layer();
@@ -201,7 +203,7 @@ size_t smoe_workspace_bytes(const smoe_layer_t* layer) {
 size_t smoe_slot_weight_bytes(const smoe_layer_t* layer) {
     if (!layer) return 0;
     const smoe_config& c = layer->cfg;
-    return (size_t)(c.K + c.spare_slots) * c.d_model * c.d_ff * smoe_elem_size(c.dtype);
+    return (size_t)(c.K + c.spare_slots) * smoe_slot_bytes(c);
 }
 
 int smoe_bind(smoe_layer_t* L, const float* router_w, void* slot_w1, void* slot_w2,
@@ -233,6 +235,8 @@ int smoe_bind(smoe_layer_t* L, const float* router_w, void* slot_w1, void* slot_
     L->d_router_split = L->workspace + w.rsplit;
     L->d_route_part = L->workspace + w.rpart;
     L->router_split_done = false;
+    L->d_router_norm = (float*)(L->workspace + w.rnorm);
+    L->router_norm_done = false;
     L->ws_ready = false;
     L->d_norm_partial = (float*)(L->workspace + w.norm);
     std::fill(L->slot_to_expert.begin(), L->slot_to_expert.end(), -1);
@@ -544,7 +548,11 @@ int smoe_update_tick(smoe_layer_t* L, const void* bank_w1, const void* bank_w2, 
 
 // ---- the hot calls: validate, then hand over to the launchers -------------
 
-static int check_hot(const smoe_layer* L, int T, const char* who, bool need_full) {
+static int check_hot(const smoe_layer* L, int T, const char* who, bool need_full) { return smoe_check_hot(L, T, who, need_full); }
+
+}  // extern "C"
+
+int smoe_check_hot(const smoe_layer* L, int T, const char* who, bool need_full) {
     if (!L) return smoe_fail(SMOE_EINVAL, "%s: null handle", who);
     if (!L->bound) return smoe_fail(SMOE_ESTATE, "%s: call smoe_bind first", who);
     if (T < 0 || T > L->cfg.max_tokens)
@@ -554,6 +562,10 @@ static int check_hot(const smoe_layer* L, int T, const char* who, bool need_full
     return SMOE_OK;
 }
 
+void smoe_note_slot_pass(smoe_layer* L) { note_slot_pass(L); }
+
+extern "C" {
+
 int smoe_route(smoe_layer_t* L, const void* x, int T, int32_t* orig_expert, float* orig_gate,
                int32_t* slot, float* gate, float* xnorm, void* stream) {
     int rc = check_hot(L, T, "smoe_route", true);
@@ -562,7 +574,7 @@ int smoe_route(smoe_layer_t* L, const void* x, int T, int32_t* orig_expert, floa
     if (!x || !orig_expert || !orig_gate || !slot || !gate || !xnorm)
         return smoe_fail(SMOE_EINVAL, "smoe_route: null buffer");
     if (misaligned(x, 16)) return smoe_fail(SMOE_EINVAL, "smoe_route: x must be 16-byte aligned");
-    if (L->cfg.dtype == SMOE_BF16 && !L->router_split_done) {
+    if (L->cfg.dtype != SMOE_F32 && !L->router_split_done) {
         rc = smoe_launch_split_router(L, as_stream(stream));
         if (rc) return rc;
         L->router_split_done = true;
@@ -618,6 +630,8 @@ int smoe_expert_ffn(smoe_layer_t* L, const void* x_perm, const int32_t* offsets,
                     void* stream) {
     int rc = check_hot(L, T, "smoe_expert_ffn", true);
     if (rc) return rc;
+    if (L->cfg.dtype == SMOE_MXFP8)
+        return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn: a layer with 8-bit slots takes 8-bit rows; use smoe_expert_ffn_mx");
     if (T == 0) return SMOE_OK;
     if (!x_perm || !offsets || !y_perm) return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn: null buffer");
     if (misaligned(x_perm, 16) || misaligned(y_perm, 16))

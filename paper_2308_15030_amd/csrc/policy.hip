@@ -66,10 +66,10 @@ int smoe_profile_memory(const smoe_config* cfg, smoe_memory_profile* out) {
     int rc = smoe_create(cfg, &tmp);                 // validates the shape
     if (rc) return rc;
     const smoe_config& c = *cfg;
-    out->expert_bytes = (uint64_t)2 * c.d_model * c.d_ff * smoe_elem_size(c.dtype);
+    out->expert_bytes = (uint64_t)2 * smoe_slot_bytes(c);
     out->resident_bytes = (uint64_t)(c.K + c.spare_slots) * out->expert_bytes;
     out->workspace_bytes = smoe_workspace_bytes(tmp);
-    out->bank_bytes = (uint64_t)c.E * out->expert_bytes;
+    out->bank_bytes = (uint64_t)c.E * 2 * c.d_model * c.d_ff * smoe_elem_size(c.dtype);
     out->router_bytes = (uint64_t)c.E * c.d_model * 4;
     smoe_destroy(tmp);
     return SMOE_OK;
@@ -109,6 +109,10 @@ int smoe_profile_end(smoe_layer_t* L, void* stream, float* elapsed_us) {
 int smoe_describe_ffn(const smoe_layer_t* L, int T, int fused, char* out, size_t n) {
     if (!L || !out || n == 0) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: null argument");
     if (T < 1 || T > L->cfg.max_tokens) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: T=%d outside [1,%d]", T, L->cfg.max_tokens);
+    if (L->cfg.dtype == SMOE_MXFP8) {
+        snprintf(out, n, "stream_mx_kernel<true, 4> | stream_mx_kernel<false, 4>");
+        return SMOE_OK;
+    }
     if (L->cfg.dtype != SMOE_BF16) return smoe_describe_ffn_f32(L, T, out, n);
     return smoe_describe_ffn_bf16(L, T, fused, out, n);
 }

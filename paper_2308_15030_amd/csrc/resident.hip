@@ -46,7 +46,7 @@ constexpr int PACK_LD = PACK_COLS + 8;       // LDS row pitch in elements (16-by
 // 64 and with 32 (55.7 GB/s; the copy engine's copy alone takes 174.5 us).  Sources in GPU memory keep a
 // workgroup per tile, for the launch is bound by memory that wants all of them, and instances without the
 // loop, which cost 3 % there (swap of 2 experts and a decode step, twice: 44.2 -> 45.8 us with it).
-constexpr int PACK_HOST_WGS = 64;
+constexpr int PACK_HOST_WGS = SMOE_PACK_HOST_WGS;
 inline unsigned pack_grid(int tiles, bool host) { return (unsigned)(host && tiles > PACK_HOST_WGS ? PACK_HOST_WGS : tiles); }
 
 __device__ __forceinline__ void pack_tile(const uint16_t* __restrict__ src, int R, int N,
@@ -273,6 +273,10 @@ int smoe_launch_pack_slot(const smoe_layer* L, int slot, const void* w1_src, con
     const smoe_config& c = L->cfg;
     const size_t per = (size_t)c.d_model * c.d_ff;               // elements per matrix
     if (map_done) *map_done = 0;
+    if (c.dtype == SMOE_MXFP8) {
+        if (map_done && map_slot >= 0) *map_done = 1;
+        return smoe_launch_pack_mx(L, slot, w1_src, w2_src, s, map_slot, expert, old_expert);
+    }
     if (c.dtype == SMOE_BF16) {
         const int nblk1 = (c.d_model / 16) * ((c.d_ff + PACK_COLS - 1) / PACK_COLS);
         const int nblk2 = (c.d_ff / 16) * ((c.d_model + PACK_COLS - 1) / PACK_COLS);
@@ -306,7 +310,7 @@ int smoe_launch_expert_norm(const smoe_layer* L, const void* w1, const void* w2,
     float* partial = L->d_norm_partial;                       // [n <= E][NORM_CHUNKS]
     size_t n16 = (size_t)c.d_model * c.d_ff * smoe_elem_size(c.dtype) / 16;
     dim3 grid(NORM_CHUNKS, n);
-    if (c.dtype == SMOE_BF16)
+    if (c.dtype != SMOE_F32)
         hipLaunchKernelGGL(sumsq_kernel<true>, grid, dim3(256), 0, s, (const uint4*)w1, (const uint4*)w2, n16, partial);
     else
         hipLaunchKernelGGL(sumsq_kernel<false>, grid, dim3(256), 0, s, (const uint4*)w1, (const uint4*)w2, n16, partial);
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(512) void stream_read_kernel(const uint4* __restric
 
 int smoe_launch_stream_read(const smoe_layer* L, int which, hipStream_t s) {
     const smoe_config& c = L->cfg;
-    const size_t n16 = (size_t)c.K * c.d_model * c.d_ff * smoe_elem_size(c.dtype) / 16;
+    const size_t n16 = (size_t)c.K * smoe_slot_bytes(c) / 16;
     const void* buf = which == 0 ? L->slot_w1 : L->slot_w2;
     int dev = 0, cus = 256;
     (void)hipGetDevice(&dev);

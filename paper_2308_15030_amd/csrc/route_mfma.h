@@ -157,27 +157,16 @@ __device__ __forceinline__ void smoe_store_choice(const smoe_route_args& a, int 
     a.xnorm[tok] = sqrtf(ss);
 }
 
-// The partial logits of the 8 waves meet in LDS and every token's results are written.
+// The partial logits of the 8 waves and the sums of squares meet in LDS, in the staged tokens' place.
+// accumulator register i of lane l: expert 8*(i/4) + 4*(l/32) + i%4 (+32 per block), token l%32
 template <int NEB, int TB>
-__device__ __forceinline__ void smoe_route_finish(const int block, const smoe_route_args& a,
-                                                  smoe_f32x16 (&acc)[smoe_route_shape<NEB, TB>::NEBH][TB], float (&sq)[TB],
-                                                  float* smem) {
+__device__ __forceinline__ void smoe_route_meet(const int E, smoe_f32x16 (&acc)[smoe_route_shape<NEB, TB>::NEBH][TB],
+                                                float (&sq)[TB], float* part, float* sqp) {
     using S = smoe_route_shape<NEB, TB>;
     constexpr int NS = S::NS, NEBH = S::NEBH, LDP = S::LDP, RT = SMOE_RT, NTOK = S::NTOK;
-    float* part = smem;                                    // [NS][NTOK][LDP] partial logits
-    float* sqp = smem + NS * NTOK * LDP;                   // [NS][2 halves][NTOK] partial sums of squares
-    __shared__ int32_t s_hist[TB * 256];                   // tokens per block and slot
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int slice = wave % NS, group = wave / NS;
-    const int tw0 = block * NTOK, neb = (a.E + 31) >> 5;
-    if (a.hist32)
-        for (int i = tid; i < TB * 256; i += 512) s_hist[i] = 0;
-    const int sub = lane & 15;                             // the 16 lanes of a token
-    int sl[smoe_route_chunks(NEB)][4];
-    smoe_route_slots<NEB>(sl, a, sub);
-
-    __syncthreads();                                       // the partial logits take the staged tokens' place
-    // accumulator register i of lane l: expert 8*(i/4) + 4*(l/32) + i%4 (+32 per block), token l%32
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int slice = wave % NS, group = wave / NS, neb = (E + 31) >> 5;
+    __syncthreads();
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb) {
         float* row = part + (slice * NTOK + tb * RT + (lane & 31)) * LDP + 4 * (lane >> 5);
@@ -192,6 +181,27 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_ro
         if (group == 0) sqp[(slice * 2 + (lane >> 5)) * NTOK + tb * RT + (lane & 31)] = sq[tb];
     }
     __syncthreads();
+}
+
+// The partial logits of the 8 waves meet in LDS and every token's results are written.
+template <int NEB, int TB>
+__device__ __forceinline__ void smoe_route_finish(const int block, const smoe_route_args& a,
+                                                  smoe_f32x16 (&acc)[smoe_route_shape<NEB, TB>::NEBH][TB], float (&sq)[TB],
+                                                  float* smem) {
+    using S = smoe_route_shape<NEB, TB>;
+    constexpr int NS = S::NS, LDP = S::LDP, RT = SMOE_RT, NTOK = S::NTOK;
+    float* part = smem;                                    // [NS][NTOK][LDP] partial logits
+    float* sqp = smem + NS * NTOK * LDP;                   // [NS][2 halves][NTOK] partial sums of squares
+    __shared__ int32_t s_hist[TB * 256];                   // tokens per block and slot
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int tw0 = block * NTOK;
+    if (a.hist32)
+        for (int i = tid; i < TB * 256; i += 512) s_hist[i] = 0;
+    const int sub = lane & 15;                             // the 16 lanes of a token
+    int sl[smoe_route_chunks(NEB)][4];
+    smoe_route_slots<NEB>(sl, a, sub);
+
+    smoe_route_meet<NEB, TB>(a.E, acc, sq, part, sqp);
 
     // epilogue: lanes 16q .. 16q + 15 of wave w own token 4w + q of every 32-token block
 #pragma unroll
@@ -242,9 +252,9 @@ __device__ __forceinline__ void smoe_add_squares(float& sq, const uint4& xv) {
 }
 
 // MULTI: d_model takes more than one chunk; the first round of the next chunk's loads is then in flight
-// while this one is multiplied.
-template <int NEB, int TB, bool MULTI>
-__device__ __forceinline__ void smoe_route_mfma_body(const int block, const smoe_route_args& a, float* smem) {
+// while this one is multiplied.  ARGS: smoe_route_args or a type derived from it with a smoe_route_finish of its own.
+template <int NEB, int TB, bool MULTI, class ARGS>
+__device__ __forceinline__ void smoe_route_mfma_body(const int block, const ARGS& a, float* smem) {
     using S = smoe_route_shape<NEB, TB>;
     constexpr int NS = S::NS, NEBH = S::NEBH, RT = SMOE_RT, NTOK = S::NTOK;
     constexpr int KC = SMOE_ROUTE_KC;
@@ -373,8 +383,8 @@ __device__ __forceinline__ void smoe_route_mfma_body(const int block, const smoe
 // A lane holds four consecutive reduction elements of its row, the two halves of the wave eight: one
 // 16-byte load per operand feeds four MFMAs.  A product of 32 x 32 x 2 takes 64 cycles, so the operands
 // come straight from memory.
-template <int NEB>
-__device__ __forceinline__ void smoe_route_f32_body(const int block, const smoe_route_args& a, float* smem) {
+template <int NEB, class ARGS>
+__device__ __forceinline__ void smoe_route_f32_body(const int block, const ARGS& a, float* smem) {
     using S = smoe_route_shape<NEB, 1>;
     constexpr int NS = S::NS, NEBH = S::NEBH;
     constexpr int G = NEBH == 1 ? 6 : NEBH == 2 ? 4 : 2;   // steps of 8 reduction elements fetched together

@@ -84,6 +84,8 @@ struct smoe_layer {
     void* d_router_split = nullptr;          // bf16 path: router weights in matrix-operand order
     void* d_route_part = nullptr;            // small batches: partial logits and sums of squares of at most SMOE_FEW_T tokens
     bool router_split_done = false;          // made by the first smoe_route after a bind
+    float* d_router_norm = nullptr;          // largest |w_e| of the router's rows (smoe_route_topk)
+    bool router_norm_done = false;           // made by the first smoe_route_topk after a bind
 
     hipEvent_t prof_ev[4] = {nullptr, nullptr, nullptr, nullptr};   // one-shot FFN profiling events
     hipEvent_t bracket[2] = {nullptr, nullptr};                     // smoe_profile_begin / _end
@@ -98,14 +100,38 @@ struct smoe_layer {
 };
 
 struct smoe_ws_layout {
-    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, stage, total;
+    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, rnorm, stage, total;
 };
 smoe_ws_layout smoe_ws_plan(const smoe_config& c);
 
 int smoe_fail(int code, const char* fmt, ...);
 int smoe_check_hip(hipError_t e, const char* what);
+// What the calls on a batch have in common: a bound handle, 0 <= T <= max_tokens and, with need_full, every slot filled.
+int smoe_check_hot(const smoe_layer* L, int T, const char* who, bool need_full);
+void smoe_note_slot_pass(smoe_layer* L);
+inline bool smoe_misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
-inline size_t smoe_elem_size(int dtype) { return dtype == SMOE_BF16 ? 2 : 4; }
+// Activations and the experts of the bank: fp32, or bf16 for every other type of layer.
+inline size_t smoe_elem_size(int dtype) { return dtype == SMOE_F32 ? 4 : 2; }
+// 8-bit operands (mx.h): steps of 64 reduction elements, their scales in groups of four; bytes of the elements and of the scales of
+// 32 rows, of one matrix [R, N] with its scales, and of the hidden activations.
+constexpr int SMOE_MX_STEP = 64;
+inline __host__ __device__ int smoe_mx_steps(int r) { return (r + SMOE_MX_STEP - 1) / SMOE_MX_STEP; }
+inline __host__ __device__ int smoe_mx_groups(int r) { return (smoe_mx_steps(r) + 3) / 4; }
+inline __host__ __device__ size_t smoe_mx_row_bytes(int r) { return (size_t)smoe_mx_steps(r) * 2048; }
+inline __host__ __device__ size_t smoe_mx_row_scales(int r) { return (size_t)smoe_mx_groups(r) * 256; }
+inline size_t smoe_mx_matrix_bytes(int R, int N) { return (size_t)(N / 32) * (smoe_mx_row_bytes(R) + smoe_mx_row_scales(R)); }
+inline size_t smoe_mx_hidden_blocks(const smoe_config& c) { return (size_t)(c.max_tokens + 31) / 32 + c.K; }   // segments re-based to 32 rows
+inline size_t smoe_mx_hidden_bytes(const smoe_config& c) {
+    return smoe_mx_hidden_blocks(c) * (smoe_mx_row_bytes(c.d_ff) + smoe_mx_row_scales(c.d_ff));
+}
+// Bytes of one slot in either of the two slot arrays.
+inline size_t smoe_slot_bytes(const smoe_config& c) {
+    if (c.dtype != SMOE_MXFP8) return (size_t)c.d_model * c.d_ff * smoe_elem_size(c.dtype);
+    const size_t a = smoe_mx_matrix_bytes(c.d_model, c.d_ff), b = smoe_mx_matrix_bytes(c.d_ff, c.d_model);
+    return a > b ? a : b;
+}
+inline size_t smoe_scale_pitch(int d) { return ((size_t)d / 32 + 7) / 8 * 8; }   // bytes of a row of scales
 // smoe_forward takes at most this many tokens through its small-batch path (decode.hip), and at most those
 // whose rows (8 elements of padding each) fit the dynamic LDS of a compute unit; the path keeps the hidden
 // activations of every slot for every token of the batch, in blocks of 32 tokens.
@@ -170,9 +196,25 @@ int smoe_describe_ffn_f32(const smoe_layer* L, int T, char* out, size_t n);
 int smoe_describe_ffn_bf16(const smoe_layer* L, int T, int fused, char* out, size_t n);
 int smoe_launch_combine(const smoe_layer* L, const void* y_perm, const int32_t* inv_perm,
                         const float* gate, const void* residual, int T, void* out, hipStream_t s);
+// k experts per token: the sorting, the weighted sum, the router; the norm in front; the products on 8-bit values
+int smoe_launch_permute_topk(const smoe_layer* L, const void* x, const int32_t* slot, int T, int k, void* x_perm, int32_t* perm,
+                             int32_t* inv_perm, int32_t* offsets, hipStream_t s);
+int smoe_launch_combine_topk(const smoe_layer* L, const void* y_perm, const int32_t* inv_perm, const float* gate, const void* residual,
+                             int T, int k, void* out, hipStream_t s);
+int smoe_launch_router_norm(const smoe_layer* L, hipStream_t s);
+int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, const float* bias, const void* x, int T, int32_t* orig_expert,
+                           float* orig_gate, int32_t* slot, float* gate, float* xnorm, hipStream_t s);
+int smoe_launch_add_norm(const smoe_layer* L, const void* x, const void* residual, const float* weight, float eps, int T, void* total,
+                         void* y, void* q, void* q_scale, hipStream_t s);
+int smoe_launch_ffn_mx(const smoe_layer* L, const void* q, const void* q_scale, const int32_t* perm, int k, const int32_t* offsets, int T,
+                       void* y_perm, hipStream_t s);
+// Workgroups of a load whose source is pinned host memory (see resident.hip)
+constexpr int SMOE_PACK_HOST_WGS = 64;
 // packs / copies one expert's two matrices into physical slot `phys`
 int smoe_launch_pack_slot(const smoe_layer* L, int slot, const void* w1_src, const void* w2_src, hipStream_t s,
                           int map_slot = -1, int expert = -1, int old_expert = -1, int* map_done = nullptr);
+int smoe_launch_pack_mx(const smoe_layer* L, int slot, const void* w1_src, const void* w2_src, hipStream_t s, int map_slot, int expert,
+                        int old_expert);
 // slot now serves `expert` from physical slot `phys` (old_expert, if any, leaves the maps)
 int smoe_launch_set_map(const smoe_layer* L, int slot, int expert, int old_expert, int phys, hipStream_t s);
 int smoe_launch_expert_norm(const smoe_layer* L, const void* w1, const void* w2, int n, float* out,

@@ -150,6 +150,7 @@ __global__ __launch_bounds__(SB) void sort_hist_kernel(const int32_t* __restrict
 
 // Position of token t = offsets[slot] + (tokens of that slot in earlier blocks)
 //                     + (in earlier waves of this block) + (in lower lanes of this wave).
+template <bool PAIRS>
 __global__ __launch_bounds__(SB) void sort_rank_kernel(const int32_t* __restrict__ slot, int T, int K,
                                                        int nblk, const int32_t* __restrict__ hist,
                                                        int32_t* __restrict__ perm,
@@ -211,6 +212,8 @@ __global__ __launch_bounds__(SB) void sort_rank_kernel(const int32_t* __restrict
         int pos = s_base[my] + s_wave[wave * K + my] + rank_in_wave;
         perm[pos] = t;
         inv_perm[t] = pos;
+    } else if (PAIRS && t < T) {
+        inv_perm[t] = -1;
     }
 }
 
@@ -354,11 +357,12 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const uint4* __restric
 constexpr int PERM_ONE_MAX = 2048, PERM_TWO_MAX = 32768, PERM_WIDE_MAX = 8192;
 constexpr size_t PERM_TWO_BYTES = (size_t)64 << 20;
 
-template <int PARTS>
+// PAIRS (smoe_permute_topk): the sorted items are (token, choice) pairs, `per` to a row of x; a pair without a slot gets position -1.
+template <int PARTS, bool PAIRS>
 __global__ __launch_bounds__(256) void permute_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ slot, int T, int K,
                                                           int chunks_per_row, uint4* __restrict__ x_perm, int32_t* __restrict__ perm,
                                                           int32_t* __restrict__ inv_perm, int32_t* __restrict__ offsets,
-                                                          const int32_t* __restrict__ hist, int nblk) {
+                                                          const int32_t* __restrict__ hist, int nblk, int per) {
     __shared__ int32_t s_total[4][256], s_before[4][256];  // per wave: tokens of each slot, and those in front of the block
     __shared__ int32_t s_pos[64];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -433,12 +437,14 @@ __global__ __launch_bounds__(256) void permute_rows_kernel(const uint4* __restri
             perm[pos] = t0 + lane;
             inv_perm[t0 + lane] = pos;
         }
+        if (PAIRS && pos < 0 && lane / PER == part && t0 + lane < T) inv_perm[t0 + lane] = -1;
     }
+    if (PAIRS && !x_perm) return;                          // the indexes alone
     __syncthreads();
     const int r0 = part * PER, rows = min(PER, T - t0 - r0);
     for (int idx = tid; idx < rows * chunks_per_row; idx += 256) {
         const int r = idx / chunks_per_row, c = idx - r * chunks_per_row, pos = s_pos[r0 + r];
-        if (pos >= 0) x_perm[(size_t)pos * chunks_per_row + c] = x[(size_t)(t0 + r0 + r) * chunks_per_row + c];
+        if (pos >= 0) x_perm[(size_t)pos * chunks_per_row + c] = x[(size_t)(PAIRS ? (t0 + r0 + r) / per : t0 + r0 + r) * chunks_per_row + c];
     }
 }
 
@@ -455,16 +461,99 @@ int launch_permute(const smoe_config& c, const void* x, const int32_t* slot, int
     if (permute_fused(c, T)) {
         const int parts = cpr >= 256 && T <= PERM_WIDE_MAX ? 16 : 4;
         const int blocks = std::max(1, (T + 63) / 64);     // T = 0 still writes offsets = 0
-        hipLaunchKernelGGL(parts == 16 ? permute_rows_kernel<16> : permute_rows_kernel<4>, dim3(parts * blocks), dim3(256), 0, s,
-                           (const uint4*)x, slot, T, K, cpr, (uint4*)x_perm, perm, inv_perm, offsets, hist, nblk);
+        hipLaunchKernelGGL((parts == 16 ? permute_rows_kernel<16, false> : permute_rows_kernel<4, false>), dim3(parts * blocks), dim3(256), 0, s,
+                           (const uint4*)x, slot, T, K, cpr, (uint4*)x_perm, perm, inv_perm, offsets, hist, nblk, 1);
     } else {
-        hipLaunchKernelGGL(sort_rank_kernel, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, T, K, nblk, hist, perm,
+        hipLaunchKernelGGL(sort_rank_kernel<false>, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, T, K, nblk, hist, perm,
                            inv_perm, offsets);
         const size_t total = (size_t)T * cpr;
         hipLaunchKernelGGL(gather_rows_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, (const uint4*)x, perm, T, cpr,
                            (uint4*)x_perm);
     }
     return smoe_check_hip(hipGetLastError(), what);
+}
+
+// ---- k choices a token (smoe_permute_topk)
+// x_perm[inv_perm[t * k + j], :] = x[t, :] for every choice j that is served: a row is read once and written to its places.
+__global__ __launch_bounds__(256) void scatter_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ inv_perm, int T, int k,
+                                                           int chunks_per_row, uint4* __restrict__ x_perm) {
+    const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= (size_t)T * chunks_per_row) return;
+    const int t = (int)(idx / chunks_per_row), c = (int)(idx % chunks_per_row), n = T * k;
+    const uint4 v = x[idx];
+    for (int j = 0; j < k; ++j) {
+        const int pos = inv_perm[t * k + j];
+        if ((unsigned)pos < (unsigned)n) x_perm[(size_t)pos * chunks_per_row + c] = v;
+    }
+}
+
+int launch_permute_pairs(const smoe_config& c, const void* x, const int32_t* slot, int T, int k, void* x_perm, int32_t* perm,
+                         int32_t* inv_perm, int32_t* offsets, int32_t* hist, hipStream_t s) {
+    const int n = T * k, K = c.K, cpr = (int)((size_t)c.d_model * smoe_elem_size(c.dtype) / 16), nblk = smoe_sort_blocks(n);
+    if (n <= PERM_ONE_MAX) hist = nullptr;
+    else hipLaunchKernelGGL(sort_hist_kernel, dim3(nblk), dim3(SB), K * sizeof(int32_t), s, slot, n, K, hist);
+    if (permute_fused(c, n) || (!x_perm && n <= PERM_TWO_MAX)) {
+        const int parts = cpr >= 256 && n <= PERM_WIDE_MAX ? 16 : 4;
+        const int blocks = std::max(1, (n + 63) / 64);     // an empty batch still writes offsets = 0
+        hipLaunchKernelGGL((parts == 16 ? permute_rows_kernel<16, true> : permute_rows_kernel<4, true>), dim3(parts * blocks), dim3(256), 0, s,
+                           (const uint4*)x, slot, n, K, cpr, (uint4*)x_perm, perm, inv_perm, offsets, hist, nblk, k);
+    } else {
+        hipLaunchKernelGGL(sort_rank_kernel<true>, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, n, K, nblk, hist, perm,
+                           inv_perm, offsets);
+        if (x_perm)
+            hipLaunchKernelGGL(scatter_rows_kernel, dim3((unsigned)(((size_t)T * cpr + 255) / 256)), dim3(256), 0, s, (const uint4*)x, inv_perm,
+                               T, k, cpr, (uint4*)x_perm);
+    }
+    return smoe_check_hip(hipGetLastError(), "smoe_permute_topk launch");
+}
+
+// out[t, :] = sum_j gate[t, j] * y_perm[inv_perm[t, j], :] (+ residual[t, :]) in fp32, choices in their order, rounded once; a choice
+// without a position adds nothing.  16 bytes of a row per thread; the rows of four choices are asked for together.
+template <bool BF16>
+__global__ __launch_bounds__(256) void combine_pairs_kernel(const uint4* __restrict__ y_perm, const int32_t* __restrict__ inv_perm,
+                                                            const float* __restrict__ gate, const uint4* __restrict__ residual, int T, int k,
+                                                            int chunks_per_row, uint4* out) {
+    constexpr int V = BF16 ? 8 : 4, U = 4;                 // values of a piece, choices together
+    const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (idx >= (size_t)T * chunks_per_row) return;
+    const int t = (int)(idx / chunks_per_row), c = (int)(idx % chunks_per_row), n = T * k;
+    float acc[V];
+    auto unpack = [](const uint4& u, float (&f)[V]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = __uint_as_float(!BF16 ? w[i & 3] : i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    };
+    const uint4 r = residual ? residual[idx] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+    for (int j0 = 0; j0 < k; j0 += U) {
+        uint4 y[U];
+        float g[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {                      // past the choices: the last again, not added
+            const int at = t * k + min(j0 + j, k - 1), pos = inv_perm[at];
+            const bool there = (unsigned)pos < (unsigned)n && j0 + j < k;
+            g[j] = there ? gate[at] : 0.f;
+            y[j] = make_uint4(0, 0, 0, 0);
+            if (there) y[j] = y_perm[(size_t)pos * chunks_per_row + c];
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            float f[V];
+            unpack(y[j], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] = fmaf(g[j], f[i], acc[i]);
+        }
+    }
+    float f[V];
+    unpack(r, f);
+    uint32_t w[4];
+    if (residual)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] += f[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = BF16 ? smoe_pack_bf16(acc[2 * i % V], acc[(2 * i + 1) % V]) : __float_as_uint(acc[i]);
+    out[idx] = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // ------------------------------------------------------------- combine
@@ -591,11 +680,25 @@ int smoe_launch_combine(const smoe_layer* L, const void* y_perm, const int32_t* 
     int cpr = (int)((size_t)L->cfg.d_model * smoe_elem_size(L->cfg.dtype) / 16);
     size_t total = (size_t)T * cpr;
     dim3 grid((unsigned)((total + 255) / 256));
-    if (L->cfg.dtype == SMOE_BF16)
+    if (L->cfg.dtype != SMOE_F32)
         hipLaunchKernelGGL(combine_kernel<true>, grid, dim3(256), 0, s, (const uint4*)y_perm, inv_perm,
                            gate, (const uint4*)residual, T, cpr, (uint4*)out);
     else
         hipLaunchKernelGGL(combine_kernel<false>, grid, dim3(256), 0, s, (const uint4*)y_perm, inv_perm,
                            gate, (const uint4*)residual, T, cpr, (uint4*)out);
     return smoe_check_hip(hipGetLastError(), "smoe_combine launch");
+}
+
+int smoe_launch_permute_topk(const smoe_layer* L, const void* x, const int32_t* slot, int T, int k, void* x_perm, int32_t* perm,
+                             int32_t* inv_perm, int32_t* offsets, hipStream_t s) {
+    return launch_permute_pairs(L->cfg, x, slot, T, k, x_perm, perm, inv_perm, offsets, L->d_sort_hist, s);
+}
+
+int smoe_launch_combine_topk(const smoe_layer* L, const void* y_perm, const int32_t* inv_perm, const float* gate, const void* residual,
+                             int T, int k, void* out, hipStream_t s) {
+    const int cpr = (int)((size_t)L->cfg.d_model * smoe_elem_size(L->cfg.dtype) / 16);
+    const dim3 grid((unsigned)(((size_t)T * cpr + 255) / 256));
+    hipLaunchKernelGGL(L->cfg.dtype != SMOE_F32 ? combine_pairs_kernel<true> : combine_pairs_kernel<false>, grid, dim3(256), 0, s,
+                       (const uint4*)y_perm, inv_perm, gate, (const uint4*)residual, T, k, cpr, (uint4*)out);
+    return smoe_check_hip(hipGetLastError(), "smoe_combine_topk launch");
 }
