@@ -9,7 +9,7 @@
 // Which experts are chosen has to be right, and a logit in fp32 is off by some 1e-7 of |x| |w|: in a batch of 16384 tokens with 8 choices of
 // 128 experts a few choices are nearer to each other than that.  So a selection also looks at the distances it decided by (between
 // consecutive choices, the last one and the next best, the last kept group and the next); where one is within an estimate of the error, the token
-// is put on a list, and the workgroup repeats it in 64 bits, product, scores and selection, from x and the router's rows in memory.
+// is put on a list, and a wave repeats it in 64 bits, products, scores and selection, from x and the router's rows in memory.
 // Without a bias, and with single experts ranking the groups, the keys are the logits themselves, of which every score is a rising
 // function.
 
@@ -21,66 +21,149 @@ struct smoe_topk_args : smoe_route_args {
     const float* bias;
     const float* wnorm;           // largest |w_e|
     int k, sigmoid, groups, kept, best, renorm, by_logit, f32;
-    float scale, err;             // err: estimated error of a logit, in units of |x| |w| 2^-24
+    int aligned;                  // a group is 4, 8, 16, 32 or 64 experts
+    float scale;
+    float err_norm, err_sum;      // estimated error of a logit in units of 2^-24: of |x| |w|, and of the sum of its slices' magnitudes
 };
 
 namespace {
-__device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + expf(-v)); }
-__device__ __forceinline__ double sigmoid_of(double v) { return 1.0 / (1.0 + exp(-v)); }
 
-// The best experts by key of one token, in its 16 lanes: lane `sub` is left with the choice number `sub` (-1: none).  Returns whether a
-// distance that decided something is at most tol (keys) or rtol (ranks of groups).  gid: group of each of the lane's experts.
-template <int EC>
-__device__ __forceinline__ bool pick_row(float (&key)[EC][4], const int (&gid)[EC][4], const smoe_topk_args& a, int sub, float tol, int& mine) {
-    bool close = false;
-    if (a.groups > 1) {
-        float rank = -INFINITY;                            // of group `sub`
+__device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + expf(-v)); }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
+__device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
+
+// The rotations and reductions of wave_ops.h in 64 bits.
+template <int N>
+__device__ __forceinline__ float row_ror(float v) { return smoe_row_ror<N>(v); }
+template <int N>
+__device__ __forceinline__ double row_ror(double v) {
+    return __hiloint2double(smoe_row_ror<N>(__double2hiint(v)), smoe_row_ror<N>(__double2loint(v)));
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+    return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true),
+                            __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true));
+}
+template <class T>
+__device__ __forceinline__ T row_max(T v) {
+    v = larger(v, row_ror<8>(v));
+    v = larger(v, row_ror<4>(v));
+    v = larger(v, row_ror<2>(v));
+    return larger(v, row_ror<1>(v));
+}
+template <class T>
+__device__ __forceinline__ T row_sum(T v) {
+    v += row_ror<8>(v);
+    v += row_ror<4>(v);
+    v += row_ror<2>(v);
+    return v + row_ror<1>(v);
+}
+
+// The best experts by key of one token, in its 16 lanes: lane `sub` is left with choice number `sub` in `mine` (-1: none).  Returns what was
+// decided by a distance of at most tol (twice that between sums of two): 1 the choices, 2 the groups.  gid: group of each of the lane's experts.
+template <class T, int EC>
+__device__ __forceinline__ int pick_row(T (&key)[EC][4], const int (&gid)[EC][4], const smoe_topk_args& a, int sub, T tol, int& mine) {
+    const T none = -INFINITY;
+    int close = 0;
+    if (a.groups > 1 && a.aligned) {
+        // Groups of 4, 8, .. 64 experts: 1, 2, .. 16 neighbouring lanes of one of the lane's packs of four, so each lane finds the rank of its
+        // own groups with the steps of one reduction, and counts the groups in front of each (16384 tokens, 8 groups of 16: 18 us
+        // less than the walk over the groups below).
+        T rank[EC];
+        const int lanes = a.E / a.groups >> 2;
+#pragma unroll
+        for (int c = 0; c < EC; ++c) {
+            const T hi0 = larger(key[c][0], key[c][1]), lo0 = smaller(key[c][0], key[c][1]);
+            const T hi1 = larger(key[c][2], key[c][3]), lo1 = smaller(key[c][2], key[c][3]);
+            T m1 = larger(hi0, hi1), m2 = larger(smaller(hi0, hi1), larger(lo0, lo1));
+            auto merge = [&](T o1, T o2) {
+                m2 = larger(smaller(m1, o1), larger(m2, o2));
+                m1 = larger(m1, o1);
+            };
+            if (lanes >= 2) merge(dpp<0xB1>(m1), dpp<0xB1>(m2));
+            if (lanes >= 4) merge(dpp<0x4E>(m1), dpp<0x4E>(m2));
+            if (lanes >= 8) merge(dpp<0x141>(m1), dpp<0x141>(m2));   // the other quad of eight lanes
+            if (lanes >= 16) merge(dpp<0x140>(m1), dpp<0x140>(m2));  // the other eight
+            rank[c] = a.best == 2 && m2 > none ? m1 + m2 : m1;
+        }
+        int ahead[EC];
+#pragma unroll
+        for (int c = 0; c < EC; ++c) ahead[c] = 0;
+        for (int s = 0; s < 16; s += lanes) {              // the row turned by s lanes: group (lane - s) / lanes of every pack
+            const int at = ((threadIdx.x - s) & 15) | (threadIdx.x & 48);
+#pragma unroll
+            for (int o = 0; o < EC; ++o) {
+                const T v = __shfl(rank[o], at);
+#pragma unroll
+                for (int c = 0; c < EC; ++c) {
+                    const bool before = o < c || (o == c && ((at ^ threadIdx.x) & 15) && (at & 15) < (int)(threadIdx.x & 15));
+                    ahead[c] += v > rank[c] || (v == rank[c] && before && (o < c || s)) ? 1 : 0;
+                }
+            }
+        }
+        T worst = INFINITY, next = none;
+#pragma unroll
+        for (int c = 0; c < EC; ++c) {
+            if (64 * c >= a.E) continue;                   // uniform
+            const bool in = 64 * c + 4 * sub < a.E;
+            const bool keep = in && ahead[c] < a.kept && rank[c] > none;
+            worst = smaller(worst, in && ahead[c] < a.kept ? rank[c] : T(INFINITY));
+            next = larger(next, in && ahead[c] >= a.kept ? rank[c] : none);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) key[c][j] = keep ? key[c][j] : none;
+        }
+        close = -row_max(-worst) - row_max(next) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;   // (two empty groups: NaN, not close)
+    } else if (a.groups > 1) {
+        T rank = none;                                     // of group `sub`
         for (int g = 0; g < a.groups; ++g) {
-            float m1 = -INFINITY, m2 = -INFINITY;          // the two largest keys of the group
+            T m1 = none, m2 = none;                        // the two largest keys of the group
 #pragma unroll
             for (int c = 0; c < EC; ++c)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float v = gid[c][j] == g ? key[c][j] : -INFINITY;
-                    m2 = fmaxf(m2, fminf(m1, v));
-                    m1 = fmaxf(m1, v);
+                    const T v = gid[c][j] == g ? key[c][j] : none;
+                    m2 = larger(m2, smaller(m1, v));
+                    m1 = larger(m1, v);
                 }
-            auto merge = [&](float o1, float o2) {
-                m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
-                m1 = fmaxf(m1, o1);
+            auto merge = [&](T o1, T o2) {
+                m2 = larger(smaller(m1, o1), larger(m2, o2));
+                m1 = larger(m1, o1);
             };
-            merge(smoe_row_ror<8>(m1), smoe_row_ror<8>(m2));
-            merge(smoe_row_ror<4>(m1), smoe_row_ror<4>(m2));
-            merge(smoe_row_ror<2>(m1), smoe_row_ror<2>(m2));
-            merge(smoe_row_ror<1>(m1), smoe_row_ror<1>(m2));
-            const float r = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
+            merge(row_ror<8>(m1), row_ror<8>(m2));
+            merge(row_ror<4>(m1), row_ror<4>(m2));
+            merge(row_ror<2>(m1), row_ror<2>(m2));
+            merge(row_ror<1>(m1), row_ror<1>(m2));
+            const T r = a.best == 2 && m2 > none ? m1 + m2 : m1;
             rank = g == sub ? r : rank;
         }
         unsigned kept = 0;
-        float last = INFINITY;
+        T last = INFINITY;
         for (int i = 0; i < a.kept; ++i) {
-            last = smoe_row_max(rank);
+            last = row_max(rank);
             const int w = smoe_row_min(rank == last ? sub : 99);
-            if (last > -INFINITY) kept |= 1u << (w & 31);
-            rank = w == sub ? -INFINITY : rank;
+            if (last > none) kept |= 1u << (w & 31);
+            rank = w == sub ? none : rank;
         }
-        const float next = smoe_row_max(rank);
-        close = last - next <= (a.best == 2 ? 2.f * tol : tol);     // (two empty groups: NaN, not close)
+        close = last - row_max(rank) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) key[c][j] = (kept >> (gid[c][j] & 31)) & 1u ? key[c][j] : -INFINITY;
+            for (int j = 0; j < 4; ++j) key[c][j] = (kept >> (gid[c][j] & 31)) & 1u ? key[c][j] : none;
     }
     mine = -1;
-    float last = INFINITY;
+    T last = INFINITY;
     for (int i = 0; i <= a.k; ++i) {                       // one round more than choices: the distance to the next best
-        float m = -INFINITY;
+        T m = none;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m = fmaxf(m, key[c][j]);
-        m = smoe_row_max(m);
-        close |= last - m <= tol;
+            for (int j = 0; j < 4; ++j) m = larger(m, key[c][j]);
+        m = row_max(m);
+        close |= last - m <= tol ? 1 : 0;
         last = m;
         if (i == a.k) break;                               // uniform
         int e = INT_MAX;
@@ -89,123 +172,188 @@ __device__ __forceinline__ bool pick_row(float (&key)[EC][4], const int (&gid)[E
 #pragma unroll
             for (int j = 3; j >= 0; --j) e = key[c][j] == m ? 64 * c + 4 * sub + j : e;
         e = smoe_row_min(e);
-        if (m > -INFINITY) mine = i == sub ? e : mine;
+        mine = m > none && i == sub ? e : mine;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) key[c][j] = 64 * c + 4 * sub + j == e ? -INFINITY : key[c][j];
+            for (int j = 0; j < 4; ++j) key[c][j] = 64 * c + 4 * sub + j == e ? none : key[c][j];
     }
     return close;
 }
 
-// Weights of the choices in the 16 lanes (w: this lane's score, 0 where it has no choice).
-__device__ __forceinline__ float weigh(float w, const smoe_topk_args& a) {
+// A selection of token tok in its 16 lanes: among the resident experts with `served`, else among all.  score_at: an expert's score.  Returns
+// what pick_row does; store: write the results to id and gate.
+template <class T, int EC, class AT>
+__device__ __forceinline__ int select_row(const smoe_topk_args& a, const T (&key)[EC][4], AT score_at, const int (&sl)[EC][4],
+                                          const int (&gid)[EC][4], int sub, int tok, bool served, int32_t* id, float* gate, bool store, T tol) {
+    T kk[EC][4];
+#pragma unroll
+    for (int c = 0; c < EC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kk[c][j] = served && sl[c][j] < 0 ? T(-INFINITY) : key[c][j];
+    int mine;
+    const int close = pick_row<T, EC>(kk, gid, a, sub, tol, mine);
+    const int e = min(max(mine, 0), a.E - 1);
+    T w = 0;
+    if (mine >= 0) w = score_at(e);
     if (a.renorm) {
-        const float sum = smoe_row_sum(w);
-        w = sum > 0.f ? w / sum : 0.f;
+        const T sum = row_sum(w);
+        w = sum > 0 ? w / sum : T(0);
     }
-    return w * a.scale;
+    if (sub < a.k && store) {
+        const size_t at = (size_t)tok * a.k + sub;
+        id[at] = !served ? e : mine < 0 ? -1 : a.e2s[e];   // (a token whose logits are all NaN: expert 0, weight 0)
+        gate[at] = (float)(w * a.scale);
+    }
+    return close;
 }
 
-__device__ __forceinline__ double wave_max(double v) {
-    for (int o = 32; o > 0; o >>= 1) v = fmax(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ double wave_sum(double v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-__device__ __forceinline__ int wave_min(int v) {
-    for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o));
-    return v;
-}
+// One token again in 64 bits, by one wave.  Only logits whose order is in question are computed again: those of experts whose keys are within
+// the tolerance of another's, those that rank a group near another where the groups are in question (`groups`), all of them where a bias meets the softmax (every key holds the sum over all).
+// The others keep their fp32 logits, which are apart from whatever they are compared with.  Few tokens come here, and a workgroup that has one is
+// the last to end, so what counts is the time of one pass, much of it instructions that come from the L2: loops are not unrolled.
+template <int EC>
+struct topk_exact {
+    static constexpr int N = 64 * EC, WAVES = EC == 4 ? 6 : 8;   // waves that work on such tokens: what fits the LDS beside the logits
+    double logit[N], score[N];                             // score: first the fp32 keys of all experts and of the resident ones
+};
 
-// The selection of one token again, by one wave, from its logits in 64 bits; experts lane, lane + 64, ...
-__device__ void pick_exact(const double* logit, const smoe_topk_args& a, bool served, int tok) {
-    const int lane = threadIdx.x & 63;
-    double v[4], s[4], key[4], top = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const int e = lane + 64 * c;
-        v[c] = e < a.E ? logit[e] : -INFINITY;
-        top = fmax(top, v[c]);
+template <int EC, class AT>
+__device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, AT logit_at, float err, bool groups, topk_exact<EC>& s) {
+    const int lane = threadIdx.x & 63, sub = lane & 15, per = a.E / a.groups;
+    const bool all = !a.sigmoid && !a.by_logit;
+    float* fkey = (float*)s.score;
+    float* rkey = fkey + 64 * EC;
+    float most = 0.f;
+#pragma unroll 1
+    for (int e = lane; e < 64 * EC; e += 64) {
+        const float l = e < a.E ? logit_at(e) : -INFINITY;
+        const float key = a.by_logit || all || e >= a.E ? l : sigmoid_of(l) + (a.bias ? a.bias[e] : 0.f);
+        s.logit[e] = l;
+        fkey[e] = key;
+        rkey[e] = e < a.E && a.e2s[e] >= 0 ? key : -INFINITY;
+        most = fmaxf(most, e < a.E ? fabsf(key) : 0.f);
     }
-    top = wave_max(top);
-    double z = 0;
+    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    const float tol = 2.f * (a.by_logit ? err : 0.25f * err + 4.8e-7f * (most + 1.f));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // lanes of a wave read what others wrote: its LDS accesses are in order
+    unsigned near_all = 0, near_res = 0;                   // groups whose rank is near another's
+    if (groups) {
+        float r[2];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        s[c] = lane + 64 * c >= a.E ? 0.0 : a.sigmoid ? sigmoid_of(v[c]) : exp(v[c] - top);
-        z += s[c];
-    }
-    z = a.sigmoid ? 1.0 : wave_sum(z);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const int e = lane + 64 * c;
-        s[c] /= z;
-        const bool ok = e < a.E && (!served || a.e2s[e < a.E ? e : 0] >= 0);
-        key[c] = !ok ? -INFINITY : a.by_logit ? v[c] : s[c] + (a.bias ? (double)a.bias[e] : 0.0);
-    }
-    const int per = a.E / a.groups;
-    if (a.groups > 1) {
-        double rank = -INFINITY;                           // of group `lane`
+        for (int res = 0; res < 2; ++res) {
+            float m1 = -INFINITY, m2 = -INFINITY;
+#pragma unroll 1
+            for (int f = 0; f < per; ++f) {
+                const float v = lane < a.groups ? (res ? rkey : fkey)[lane * per + f] : -INFINITY;
+                m2 = fmaxf(m2, fminf(m1, v));
+                m1 = fmaxf(m1, v);
+            }
+            r[res] = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
+        }
+#pragma unroll 1
         for (int g = 0; g < a.groups; ++g) {
-            double m1 = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) m1 = fmax(m1, (lane + 64 * c) / per == g ? key[c] : -INFINITY);
-            m1 = wave_max(m1);
-            int first = INT_MAX;                           // one expert that holds it is left out of the second
-#pragma unroll
-            for (int c = 0; c < 4; ++c) first = min(first, (lane + 64 * c) / per == g && key[c] == m1 ? lane + 64 * c : INT_MAX);
-            first = wave_min(first);
-            double m2 = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) m2 = fmax(m2, (lane + 64 * c) / per == g && lane + 64 * c != first ? key[c] : -INFINITY);
-            m2 = wave_max(m2);
-            const double r = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
-            rank = g == lane ? r : rank;
+            const float o0 = __shfl(r[0], g), o1 = __shfl(r[1], g);
+            near_all |= lane != g && fabsf(r[0] - o0) <= 2.f * tol;
+            near_res |= lane != g && fabsf(r[1] - o1) <= 2.f * tol;
         }
-        unsigned kept = 0;
-        for (int i = 0; i < a.kept; ++i) {
-            const double m = wave_max(rank);
-            const int w = wave_min(rank == m ? lane : 99);
-            if (m > -INFINITY) kept |= 1u << (w & 31);
-            rank = w == lane ? -INFINITY : rank;
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) key[c] = (kept >> (((lane + 64 * c) / per) & 31)) & 1u ? key[c] : -INFINITY;
+        near_all = (unsigned)__ballot(lane < a.groups && near_all);
+        near_res = (unsigned)__ballot(lane < a.groups && near_res);
     }
-    int mine = -1;
-    double w = 0;
-    for (int i = 0; i < a.k; ++i) {
-        double m = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) m = fmax(m, key[c]);
-        m = wave_max(m);
-        int e = INT_MAX;
-#pragma unroll
-        for (int c = 3; c >= 0; --c) e = key[c] == m ? lane + 64 * c : e;
-        e = wave_min(e);
-        double sc = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            sc = fmax(sc, lane + 64 * c == e ? s[c] : 0.0);
-            key[c] = lane + 64 * c == e ? -INFINITY : key[c];
+#pragma unroll 1
+    for (int e0 = 0; e0 < a.E; e0 += 64) {
+        const int e = e0 + lane;
+        bool again = e < a.E;
+        if (!all) {
+            const float mine = fkey[e];
+            int near = 0;
+#pragma unroll 1
+            for (int f = 0; f < a.E; f += 4) {             // itself among them; past E: infinitely far
+                const float4 o = *(const float4*)(fkey + f);
+                near += (fabsf(mine - o.x) <= tol) + (fabsf(mine - o.y) <= tol) + (fabsf(mine - o.z) <= tol) + (fabsf(mine - o.w) <= tol);
+            }
+            bool top = false;
+            if (groups && again) {
+                const int f0 = e / per * per;
+                int above = 0, above_res = 0;
+#pragma unroll 1
+                for (int f = f0; f < f0 + per; ++f) {
+                    above += fkey[f] > mine;
+                    above_res += rkey[f] > mine;
+                }
+                const int g = e / per;
+                top = ((near_all >> g & 1) && above < a.best) || ((near_res >> g & 1) && rkey[e] == mine && above_res < a.best);
+            }
+            again = again && (near > 1 || top);
         }
-        sc = wave_max(sc);
-        if (m > -INFINITY && lane == i) { mine = e; w = sc; }
-    }
-    const double sum = wave_sum(w);
-    if (a.renorm) w = sum > 0 ? w / sum : 0;
-    if (lane < a.k) {
-        const size_t at = (size_t)tok * a.k + lane;
-        if (served) {
-            a.slot[at] = mine < 0 ? -1 : a.e2s[mine];
-            a.gate[at] = (float)(w * a.scale);
-        } else {
-            a.orig_expert[at] = max(mine, 0);
-            a.orig_gate[at] = (float)(w * a.scale);
+        unsigned long long todo = __ballot(again);
+#pragma unroll 1
+        while (todo) {                                     // two experts at a time
+            const int e1 = e0 + __ffsll(todo) - 1;
+            todo &= todo - 1;
+            const int e2 = todo ? e0 + __ffsll(todo) - 1 : e1;
+            todo &= todo - 1;
+            const float *w1 = a.wrow + (size_t)e1 * a.d, *w2 = a.wrow + (size_t)e2 * a.d;
+            double s1 = 0, s2 = 0;
+#pragma unroll 2
+            for (int c = lane * 4; c < a.d; c += 256) {    // d_model is a multiple of 4
+                const float4 u = *(const float4*)(w1 + c), v = *(const float4*)(w2 + c);
+                float4 x;
+                if (a.f32) x = *(const float4*)((const float*)a.x + (size_t)tok * a.d + c);
+                else {
+                    const uint2 p = *(const uint2*)((const uint16_t*)a.x + (size_t)tok * a.d + c);
+                    x = make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16),
+                                    __uint_as_float(p.y & 0xFFFF0000u));
+                }
+                s1 = fma((double)x.x, (double)u.x, s1); s2 = fma((double)x.x, (double)v.x, s2);
+                s1 = fma((double)x.y, (double)u.y, s1); s2 = fma((double)x.y, (double)v.y, s2);
+                s1 = fma((double)x.z, (double)u.z, s1); s2 = fma((double)x.z, (double)v.z, s2);
+                s1 = fma((double)x.w, (double)u.w, s1); s2 = fma((double)x.w, (double)v.w, s2);
+            }
+#pragma unroll 1
+            for (int o = 1; o < 64; o <<= 1) {
+                s1 += __shfl_xor(s1, o);
+                s2 += __shfl_xor(s2, o);
+            }
+            if (lane == 0) { s.logit[e1] = s1; s.logit[e2] = s2; }
         }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double top = 0, z = 0;                                 // scores: the largest logit, then the sum of the exponentials
+    if (!a.sigmoid) {
+        top = -INFINITY;
+#pragma unroll 1
+        for (int e = lane; e < a.E; e += 64) top = fmax(top, s.logit[e]);
+#pragma unroll 1
+        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+    }
+#pragma unroll 1
+    for (int e = lane; e < 64 * EC; e += 64) {
+        const double p = e >= a.E ? 0.0 : exp(a.sigmoid ? -s.logit[e] : s.logit[e] - top);
+        s.score[e] = a.sigmoid ? 1.0 / (1.0 + p) : p;
+        z += p;
+    }
+    if (!a.sigmoid) {
+#pragma unroll 1
+        for (int o = 1; o < 64; o <<= 1) z += __shfl_xor(z, o);
+    }
+    const double inv_z = a.sigmoid ? 1.0 : 1.0 / z;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double key[EC][4];
+    int sl[EC][4], gid[EC][4];
+#pragma unroll
+    for (int c = 0; c < EC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 64 * c + 4 * sub + j, ei = min(e, a.E - 1);
+            key[c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
+            key[c][j] = e < a.E ? key[c][j] : -INFINITY;
+            sl[c][j] = e < a.E ? a.e2s[ei] : -1;
+            gid[c][j] = e / per;
+        }
+    // the first 16 lanes select among all experts, the next 16 among the resident ones
+    select_row<double, EC>(a, key, [&](int e) { return s.score[e] * inv_z; }, sl, gid, sub, tok, lane & 16,
+                           lane & 16 ? a.slot : a.orig_expert, lane & 16 ? a.gate : a.orig_gate, lane < 32, 0.0);
 }
 
 }  // namespace
@@ -218,8 +366,10 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
     constexpr int NS = S::NS, LDP = S::LDP, NTOK = S::NTOK, EC = smoe_route_chunks(NEB), EP = NEB * 32;
     float* part = smem;                                    // [NS][NTOK][LDP] partial logits
     float* sqp = smem + NS * NTOK * LDP;                   // [NS][2 halves][NTOK] partial sums of squares
-    __shared__ int32_t s_n, s_close[NTOK];                 // tokens to be repeated in 64 bits
-    __shared__ double s_logit[256];
+    __shared__ int32_t s_n, s_close[NTOK];                 // tokens of the block to be repeated in 64 bits; bit 8: the groups too
+    __shared__ float s_err[NTOK];
+    using X = topk_exact<EC>;
+    __shared__ X s_exact[X::WAVES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 15;
     const int tw0 = block * NTOK, per = a.E / a.groups;
     if (tid == 0) s_n = 0;
@@ -231,51 +381,48 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int e = 64 * c + 4 * sub + j;
-            gid[c][j] = a.groups > 1 ? e / per : 0;
+            gid[c][j] = e / per;
             bias[c][j] = a.bias && e < a.E ? a.bias[e] : 0.f;
         }
     const float wnorm = *a.wnorm;
     smoe_route_meet<NEB, TB>(a.E, acc, sq, part, sqp);
 
-#pragma unroll
     for (int tb = 0; tb < TB; ++tb) {
         const int t = tb * SMOE_RT + wave * 4 + (lane >> 4), tok = tw0 + t;
         const float* row = part + t * LDP;
-        auto logit_at = [&](int e) {                       // fixed order of the slices
-            float s = row[e];
-#pragma unroll
-            for (int q = 1; q < NS; ++q) s += row[q * NTOK * LDP + e];
-            return s;
-        };
-        float v[EC][4], top = -INFINITY, big = 0.f;
+        float v[EC][4], big = 0.f;
 #pragma unroll
         for (int c = 0; c < EC; ++c) {
             const float* col = row + min(64 * c + 4 * sub, EP - 4);
-            float4 s = *(const float4*)col;
+            float s[4] = {0.f, 0.f, 0.f, 0.f}, m[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = 1; q < NS; ++q) {
+            for (int q = 0; q < NS; ++q) {                 // fixed order of the slices
                 const float4 o = *(const float4*)(col + q * NTOK * LDP);
-                s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w;
+                const float p[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[j] = q ? s[j] + p[j] : p[j];
+                    m[j] += fabsf(p[j]);
+                }
             }
-            v[c][0] = s.x; v[c][1] = s.y; v[c][2] = s.z; v[c][3] = s.w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bool in = 64 * c + 4 * sub + j < a.E;
-                v[c][j] = in ? v[c][j] : -INFINITY;
-                top = fmaxf(top, v[c][j]);
-                big = fmaxf(big, in ? fabsf(v[c][j]) : 0.f);
+                v[c][j] = in ? s[j] : -INFINITY;
+                big = fmaxf(big, in ? m[j] : 0.f);
             }
         }
-        top = smoe_row_max(top);
-        big = smoe_row_max(big);
         float ss = 0.f;
 #pragma unroll
         for (int q = 0; q < 2 * NS; ++q) ss += sqp[t + q * NTOK];
         const float xnorm = sqrtf(ss);
-        // error of a logit: roundings of partial sums, which are some |x| |w| / sqrt(d) for tokens that point nowhere in particular and grow to
-        // the logit's own size for those that do (a.err counts the former, 16 roundings' worth of the largest logit the latter)
-        float tol = 5.96e-8f * (a.err * xnorm * wnorm + 16.f * big);
-        float z = 1.f;
+        const float err = 0x1p-24f * (a.err_norm * xnorm * wnorm + a.err_sum * smoe_row_max(big));
+        float top = -INFINITY, z = 1.f;
+#pragma unroll
+        for (int c = 0; c < EC; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, v[c][j]);
+        top = smoe_row_max(top);
         if (!a.sigmoid) {
             z = 0.f;
 #pragma unroll
@@ -285,11 +432,17 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             z = smoe_row_sum(z);
         }
         const float inv_z = 1.f / z;
-        float key[EC][4];
+        auto logit_at = [&](int e) {
+            float s = row[e];
 #pragma unroll
-        for (int c = 0; c < EC; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) key[c][j] = v[c][j];
+            for (int q = 1; q < NS; ++q) s += row[q * NTOK * LDP + e];
+            return s;
+        };
+        auto score_at = [&](int e) {
+            const float l = logit_at(e);
+            return a.sigmoid ? sigmoid_of(l) : expf(l - top) * inv_z;
+        };
+        float tol = err;
         if (!a.by_logit) {
             float most = 0.f;
 #pragma unroll
@@ -298,62 +451,35 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
                 for (int j = 0; j < 4; ++j) {
                     const bool in = 64 * c + 4 * sub + j < a.E;
                     const float s = a.sigmoid ? sigmoid_of(v[c][j]) : expf(v[c][j] - top) * inv_z;
-                    key[c][j] = in ? s + bias[c][j] : -INFINITY;
-                    most = fmaxf(most, in ? fmaxf(fabsf(key[c][j]), s) : 0.f);
+                    v[c][j] = in ? s + bias[c][j] : -INFINITY;
+                    most = fmaxf(most, in ? fmaxf(fabsf(v[c][j]), s) : 0.f);
                 }
-            most = smoe_row_max(most);
-            // a sigmoid is at most a quarter as far off as its logit, a share of a softmax at most twice its own size times that; and the
-            // exponential, the quotient and the sum with the bias are rounded
-            tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * tol + 4.8e-7f * most;
+            // a sigmoid is off by at most a quarter of its logit's error, a share of a softmax by at most twice its own size times that; and the
+            // exponential, the quotient and the sum with the bias are rounded, each by a few units of 2^-24
+            tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + 4.8e-7f * smoe_row_max(most);
         }
-        bool close = false;
-#pragma unroll
-        for (int served = 0; served < 2; ++served) {
-            float kk[EC][4];
-#pragma unroll
-            for (int c = 0; c < EC; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) kk[c][j] = served && sl[c][j] < 0 ? -INFINITY : key[c][j];
-            int mine;
-            close |= pick_row<EC>(kk, gid, a, sub, 2.f * tol, mine);
-            float w = 0.f;
-            const int e = min(max(mine, 0), a.E - 1);
-            if (mine >= 0) {
-                const float l = logit_at(e);
-                w = a.sigmoid ? sigmoid_of(l) : expf(l - top) * inv_z;
-            }
-            w = weigh(w, a);
-            if (sub < a.k && tok < a.T) {
-                const size_t at = (size_t)tok * a.k + sub;
-                if (served) {
-                    a.slot[at] = mine < 0 ? -1 : a.e2s[e];
-                    a.gate[at] = w;
-                } else {                                   // (a token whose logits are all NaN: expert 0, weight 0)
-                    a.orig_expert[at] = e;
-                    a.orig_gate[at] = w;
-                    a.xnorm[at] = xnorm;
-                }
-            }
+        int close = select_row<float, EC>(a, v, score_at, sl, gid, sub, tok, false, a.orig_expert, a.orig_gate, tok < a.T, 2.f * tol);
+        close |= select_row<float, EC>(a, v, score_at, sl, gid, sub, tok, true, a.slot, a.gate, tok < a.T, 2.f * tol);
+        if (sub < a.k && tok < a.T) a.xnorm[(size_t)tok * a.k + sub] = xnorm;
+        if (close && sub == 0 && tok < a.T) {
+            const int i = atomicAdd(&s_n, 1);              // the order does not matter
+            s_close[i] = t | (close & 2 ? 1 << 8 : 0);
+            s_err[i] = err;
         }
-        if (close && sub == 0 && tok < a.T) s_close[atomicAdd(&s_n, 1)] = tok;   // the order does not matter
     }
     __syncthreads();
-    for (int i = 0; i < s_n; ++i) {
-        const int tok = s_close[i];
-        for (int e = wave; e < a.E; e += 8) {
-            double sum = 0;
-            const float* w = a.wrow + (size_t)e * a.d;
-            for (int c = lane; c < a.d; c += 64) {
-                const float xv = a.f32 ? ((const float*)a.x)[(size_t)tok * a.d + c]
-                                       : __uint_as_float((uint32_t)((const uint16_t*)a.x)[(size_t)tok * a.d + c] << 16);
-                sum = fma((double)xv, (double)w[c], sum);
-            }
-            sum = wave_sum(sum);
-            if (lane == 0) s_logit[e] = sum;
-        }
-        __syncthreads();
-        if (wave < 2) pick_exact(s_logit, a, wave == 1, tok);
-        __syncthreads();
+    const int n = s_n;
+    if (wave >= X::WAVES) return;
+    for (int i = wave; i < n; i += X::WAVES) {             // a wave each
+        const int word = __builtin_amdgcn_readfirstlane(s_close[i]), t = word & 255;
+        const float* row = part + t * LDP;
+        auto logit_at = [&](int e) {
+            float s = row[e];
+#pragma unroll
+            for (int q = 1; q < NS; ++q) s += row[q * NTOK * LDP + e];
+            return s;
+        };
+        choose_exact<EC>(a, tw0 + t, logit_at, s_err[i], word >> 8, s_exact[wave]);
     }
 }
 
@@ -445,7 +571,15 @@ int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, cons
     a.renorm = rule.renorm; a.scale = rule.scale;
     a.by_logit = !bias && (rule.groups == 1 || rule.group_best == 1);
     a.f32 = c.dtype == SMOE_F32;
-    a.err = 4.f;
+    const int per = c.E / rule.groups;
+    a.aligned = per >= 4 && per <= 64 && !(per & (per - 1));
+    // The partial sums of a logit pass through n roundings.  Where x points nowhere in particular they are small, and the error measured at
+    // most 0.75 |x| |w| 2^-24 (bf16; fp32: 1.3) in batches of 16384 tokens, 64 .. 16384 columns and up to 256 experts.  Where x follows a row of the
+    // router they grow to the logit's own size (seen in the slices' sums also where these cancel), and it measured 0.08 n of it.
+    const int slices = c.E <= 32 ? 8 : 4;
+    const int n = a.f32 ? 4 * (((c.d_model + 7) / 8 + slices - 1) / slices) : 3 * ((c.d_model / 16 + slices - 1) / slices);
+    a.err_norm = a.f32 ? 1.5f : 1.f;
+    a.err_sum = 1.f + 0.1f * n;
     if (c.E <= 32) return launch<1>(a, s);
     if (c.E <= 64) return launch<2>(a, s);
     if (c.E <= 128) return launch<4>(a, s);
