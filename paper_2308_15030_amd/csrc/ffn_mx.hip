@@ -140,10 +140,9 @@ __device__ __forceinline__ void store_rows(const MxArgs& g, const f32x16& acc, i
     }
 }
 
-// The four scale bytes of a group of four steps that belong to this lane's half, of a token's row of scale bytes.
-__device__ __forceinline__ uint32_t row_scales(const uint8_t* row, int group, int blocks) {
-    const uint2 v = *(const uint2*)(row + group * 8);
-    const int left = blocks - group * 8;                       // bytes behind the row's last block are not used: whatever lies there
+// The four scale bytes of a group of four steps that belong to this lane's half, of the group's eight in a row of scale bytes; `left`: blocks
+// of the row from the group on.  Bytes behind the row's last block are not used, whatever lies there.
+__device__ __forceinline__ uint32_t half_scales(uint2 v, int left) {
     uint32_t s = __builtin_amdgcn_perm(v.y, v.x, (threadIdx.x & 32) ? 0x07050301u : 0x06040200u);
     const int mine = (left + ((threadIdx.x & 32) ? 0 : 1)) >> 1;   // blocks of this half
     if (mine < 4) s &= mine > 0 ? (1u << (8 * mine)) - 1u : 0u;
@@ -204,7 +203,7 @@ __global__ __launch_bounds__(256) void stream_mx_kernel(const MxArgs g) {
                 }
             }
             const uint32_t ws = wsp[(s0 >> 2) * 64];
-            const uint32_t xs = FIRST ? row_scales(xsrow, s0 >> 2, blocks) : *(const uint32_t*)(xsrow + (s0 >> 2) * 256);
+            const uint32_t xs = FIRST ? half_scales(*(const uint2*)(xsrow + (s0 >> 2) * 8), blocks - (s0 >> 2) * 8) : *(const uint32_t*)(xsrow + (s0 >> 2) * 256);
             smoe_mx_mfma<0>(acc, w[0], x[0], ws, xs);
             if (s0 + 1 < hi) smoe_mx_mfma<1>(acc, w[1], x[1], ws, xs);
             if (s0 + 2 < hi) smoe_mx_mfma<2>(acc, w[2], x[2], ws, xs);
@@ -225,6 +224,259 @@ __global__ __launch_bounds__(256) void stream_mx_kernel(const MxArgs g) {
     if (!on) return;
     if (FIRST) store_hidden(g, acc, rb, fb);
     else store_rows(g, acc, m0 + (lane & 31), m0 + (lane & 31) < m_end, fb * 32);
+}
+
+// ------------------------------------------------------------------ many rows a slot
+// Tile = at most 256 features (8 blocks of 32) x at most 32 * TBK tokens, both operands staged through a ring of ST stages in LDS, one step of 64
+// reduction elements a stage.  Four waves: wave (wf, wt) multiplies four feature blocks with the token blocks of parity wt.  Loads go from
+// memory to LDS without passing through registers, ST - 1 steps ahead; each wave issues the same number of them a step, so that one count says
+// what has landed.  The scales of four steps come the same way, in front of the first step's operands.
+extern __shared__ __align__(16) char mx_lds[];
+constexpr int MX_BLK = 2048;              // bytes of a block of one step
+
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint32_t lds_addr(uint32_t off) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(mx_lds + off);
+}
+// Loads from memory to LDS: lane l's 16 (4) bytes land at off + 16 l (4 l), for the lanes of the mask.  Written out because the compiler, which
+// cannot tell where the builtin's data lands, would wait for every load in flight before each LDS read.  They have no result registers;
+// whoever reads the data counts them (wait_vm) and then passes a barrier.  Nothing else in the kernel uses m0.
+__device__ __forceinline__ void dma_16(const void* src, uint32_t off, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %2\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b64 exec, -1" ::"s"(lds_addr(off)), "v"(src), "s"(lanes) : "memory");
+}
+__device__ __forceinline__ void dma_4(const void* src, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr(off)), "v"(src) : "memory");
+}
+// Two kilobytes that lie linear in memory (the offset moves both sides).
+__device__ __forceinline__ void dma_2k(const char* base, uint32_t lane16, uint32_t off, uint64_t lanes) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024\n\t"
+                 "s_mov_b64 exec, -1" ::"s"(lds_addr(off)), "v"(lane16), "s"(base), "s"(lanes) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {   // at most the N youngest vector memory operations of this wave are outstanding
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <int TBK, int ST>
+struct TileShape {
+    static constexpr uint32_t STAGE = (8 + TBK) * MX_BLK;
+    static constexpr uint32_t SC = ST * STAGE;             // scales of two groups: weights [8][256], tokens [TBK][256]
+    static constexpr uint32_t SCG = (8 + TBK) * 256;
+    static constexpr size_t LDS = SC + 2 * SCG;
+};
+
+template <bool FIRST, int TBK, int ST>
+__global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const MxArgs g) {
+    using S = TileShape<TBK, ST>;
+    constexpr int TW = TBK / 4;                            // token blocks that a wave loads
+    constexpr int NBW = TBK / 2;                           // token blocks that a wave multiplies
+    constexpr int PER = 4 + 2 * TW, NSC = FIRST ? 1 + TW : 2;   // loads of a wave a step, and of the scales a group
+    const int tid = threadIdx.x, wave = uni(tid >> 6), lane = tid & 63;
+    const int wf = wave & 1, wt = wave >> 1;
+    const int nfb = g.N >> 5, ftiles = (nfb + 7) >> 3;
+    // This workgroup's item.  Row tiles of all slots in slot order; inside a slot the row tile fastest (first product) or the feature tile.  The
+    // dies take an eighth of the list each (workgroups are dealt to them in turn), so that few slots' weights pass through an L2.
+    int tiles_all = 0;
+    for (int base = 0; base < g.nslots; base += 64) {
+        const int k = base + lane;
+        int len = 0;
+        if (k < g.nslots) {
+            const int a = min(max(g.offsets[k], 0), g.rows);
+            len = max(min(max(g.offsets[k + 1], 0), g.rows), a) - a;
+        }
+        tiles_all += __builtin_amdgcn_readlane(smoe_wave_incl_scan(((len + 31) / 32 + TBK - 1) / TBK), 63);
+    }
+    const int G = tiles_all * ftiles, die = blockIdx.x % 8;
+    const int lo = (int)((long long)G * die / 8), hi = (int)((long long)G * (die + 1) / 8), item = lo + blockIdx.x / 8;
+    if (item >= hi) return;
+    int slot = 0, seg_a = 0, seg_b = 0, first = 0, pad = 0, tiles = 1;
+    {
+        int before = 0, pad_before = 0;
+        for (int base = 0; base < g.nslots; base += 64) {
+            const int k = base + lane;
+            int a = 0, b = 0;
+            if (k < g.nslots) {
+                a = min(max(g.offsets[k], 0), g.rows);
+                b = max(min(max(g.offsets[k + 1], 0), g.rows), a);
+            }
+            const int blocks = (b - a + 31) >> 5, n = (blocks + TBK - 1) / TBK;
+            const int incl = smoe_wave_incl_scan(n), pincl = smoe_wave_incl_scan(blocks);
+            const int all = __builtin_amdgcn_readlane(incl, 63);
+            if (item < (before + all) * ftiles) {          // uniform: the slot is among these 64
+                const int l = __popcll(__ballot((before + incl) * ftiles <= item));   // slots that end in front of the item
+                slot = base + l;
+                seg_a = __builtin_amdgcn_readlane(a, l);
+                seg_b = __builtin_amdgcn_readlane(b, l);
+                tiles = __builtin_amdgcn_readlane(n, l);
+                first = before + __builtin_amdgcn_readlane(incl, l) - tiles;
+                pad = pad_before + __builtin_amdgcn_readlane(pincl - blocks, l);
+                break;
+            }
+            before += all;
+            pad_before += __builtin_amdgcn_readlane(pincl, 63);
+        }
+    }
+    const int local = item - first * ftiles;
+    const int ft = FIRST ? local / tiles : local % ftiles, rt = FIRST ? local % tiles : local / ftiles;
+    const int nbk = (seg_b - seg_a + 31) >> 5, bq = nbk / tiles, br = nbk - bq * tiles;     // rows and features are cut evenly
+    const int b0 = rt * bq + min(rt, br), nb = bq + (rt < br ? 1 : 0);
+    const int m0 = seg_a + 32 * b0, pb0 = pad + b0;
+    const int fq = nfb / ftiles, fr = nfb - fq * ftiles, fb0 = ft * fq + min(ft, fr), width = fq + (ft < fr ? 1 : 0);
+    const int steps = smoe_mx_steps(g.R), blocks = g.R >> 5;
+
+    // load side
+    const char* wslot = (const char*)g.w + (size_t)g.phys[slot] * g.wstride;
+    const size_t rowb = smoe_mx_row_bytes(g.R), rows_ = smoe_mx_row_scales(g.R);
+    const uint32_t lane16 = lane * 16;
+    const char* wsrc[2];
+    uint64_t wlanes[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int f = 2 * wave + i;
+        wlanes[i] = f < width ? ~0ull : 1;                 // a block that is not there: one lane's load, so that the counts stay
+        wsrc[i] = wslot + (size_t)(fb0 + min(f, width - 1)) * rowb;
+    }
+    const char* wscale = wslot + (size_t)nfb * rowb + (size_t)(fb0 + min(2 * wave + ((lane >> 4) & 1), width - 1)) * rows_ + (lane & 15) * 16;
+    const char *tsrc[TW][2], *tscale[TW];                  // FIRST: this lane's two rows; else scalar bases (tsrc[.][0])
+    uint64_t tlanes[TW];
+#pragma unroll
+    for (int i = 0; i < TW; ++i) {
+        const int b = TW * wave + i;
+        tlanes[i] = b < nb ? ~0ull : 1;
+        const int bc = min(b, nb - 1);
+        if (FIRST) {
+            // rows of 64 bytes whose four units are permuted by (row / 2) % 4: operand reads of neighbouring lanes hit all banks
+            const uint32_t u = (lane & 3) ^ ((lane >> 3) & 3);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int t = token_of_row(g, min(m0 + bc * 32 + h * 16 + (lane >> 2), seg_b - 1));
+                tsrc[i][h] = (const char*)g.x + (size_t)t * g.R + u * 16;
+            }
+            const int t = token_of_row(g, min(m0 + bc * 32 + (lane & 31), seg_b - 1));
+            tscale[i] = (const char*)g.xs + (size_t)t * g.pitch + (lane >> 5) * 4;
+        } else {
+            tsrc[i][0] = (const char*)g.x + (size_t)(pb0 + bc) * rowb;
+            tscale[i] = nullptr;
+        }
+    }
+    const char* hscale = FIRST ? nullptr : (const char*)g.xs + (size_t)(pb0 + min(TW * wave + (lane >> 4) % TW, nb - 1)) * rows_ + (lane & 15) * 16;
+    uint32_t lst = 0;
+    auto issue = [&](int c) {                              // loads of step c into stage lst; past the last: one lane's, nowhere read
+        const bool in = c < steps;
+        if ((c & 3) == 0) {
+            const uint32_t sc = S::SC + ((c >> 2) & 1) * S::SCG;
+            const int gr = min(c >> 2, smoe_mx_groups(g.R) - 1);
+            dma_16(wscale + (size_t)gr * 256, sc + wave * 512, 0xffffffffull);
+            if (FIRST) {
+#pragma unroll
+                for (int i = 0; i < TW; ++i) dma_4(tscale[i] + gr * 8, sc + 2048 + (TW * wave + i) * 256);
+            } else {
+                dma_16(hscale + (size_t)gr * 256, sc + 2048 + wave * TW * 256, TW == 1 ? 0xffffull : 0xffffffffull);
+            }
+        }
+        const int cc = in ? c : steps - 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            dma_2k(wsrc[i] + (size_t)cc * MX_BLK, lane16, lst + (2 * wave + i) * MX_BLK, in ? wlanes[i] : 1);
+#pragma unroll
+        for (int i = 0; i < TW; ++i) {
+            const uint32_t at = lst + (8 + TW * wave + i) * MX_BLK;
+            if (FIRST) {
+                // a row that ends in the middle of the step: its last 32 bytes again, which meet zeros
+                const int u = (lane & 3) ^ ((lane >> 3) & 3);
+                const int back = cc * 64 + 32 >= g.R && u >= 2 ? 32 : 0;
+                dma_16(tsrc[i][0] + cc * 64 - back, at, in ? tlanes[i] : 1);
+                dma_16(tsrc[i][1] + cc * 64 - back, at + 1024, in ? tlanes[i] : 1);
+            } else {
+                dma_2k(tsrc[i][0] + (size_t)cc * MX_BLK, lane16, at, in ? tlanes[i] : 1);
+            }
+        }
+        lst = lst == (ST - 1) * S::STAGE ? 0 : lst + S::STAGE;
+    };
+
+    f32x16 acc[4][NBW];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < NBW; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+    uint32_t cst = 0;
+    uint32_t ws[4], ts[NBW];
+    const uint32_t toff0 = FIRST ? (lane & 31) * 64 + (((lane >> 5) ^ ((lane >> 1) & 3)) * 16) : lane16;
+    const uint32_t toff1 = FIRST ? (lane & 31) * 64 + (((2 + (lane >> 5)) ^ ((lane >> 1) & 3)) * 16) : lane16 + 1024;
+    auto step = [&](auto uc, int c) {
+        constexpr int u = decltype(uc)::value;
+        if (u == 0) {
+            const uint32_t sc = S::SC + ((c >> 2) & 1) * S::SCG;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) ws[a] = *(const uint32_t*)(mx_lds + sc + (wf * 4 + a) * 256 + lane * 4);
+#pragma unroll
+            for (int b = 0; b < NBW; ++b) {
+                const char* p = mx_lds + sc + 2048 + (2 * b + wt) * 256;
+                if (FIRST) {
+                    const uint32_t x = *(const uint32_t*)(p + (lane & 31) * 4), y = *(const uint32_t*)(p + 128 + (lane & 31) * 4);
+                    ts[b] = half_scales(make_uint2(x, y), blocks - (c >> 2) * 8);
+                } else {
+                    ts[b] = *(const uint32_t*)(p + lane * 4);
+                }
+            }
+        }
+        uint4 wv[4][2], tv[NBW][2];
+#pragma unroll
+        for (int b = 0; b < NBW; ++b) {
+            const char* p = mx_lds + cst + (8 + 2 * b + wt) * MX_BLK;
+            tv[b][0] = *(const uint4*)(p + toff0);
+            tv[b][1] = *(const uint4*)(p + toff1);
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const char* p = mx_lds + cst + (wf * 4 + a) * MX_BLK + lane16;
+            wv[a][0] = *(const uint4*)p;
+            wv[a][1] = *(const uint4*)(p + 1024);
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int b = 0; b < NBW; ++b) smoe_mx_mfma<u>(acc[a][b], wv[a], tv[b], ws[a], ts[b]);
+        cst = cst == (ST - 1) * S::STAGE ? 0 : cst + S::STAGE;
+    };
+    // Step c + 1 has landed: what may be outstanding are the loads of the ST - 2 steps behind it.
+    auto landed = [&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+        constexpr int younger = (ST - 2) * PER + ((u + 2) % 4 == 0 || (ST > 3 && (u + 3) % 4 == 0) ? NSC : 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // this wave's reads of the stage that is loaded next are done
+        wait_vm<younger>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+#pragma unroll 1
+    for (int c = 0; c < ST - 1; ++c) issue(c);
+    landed(std::integral_constant<int, 3>{});              // step 0: behind it lie steps 1 .. ST - 2, none the first of a group
+    for (int c = 0; c < steps; c += 4) {
+        auto one = [&](auto uc) {
+            constexpr int u = decltype(uc)::value;
+            issue(c + u + ST - 1);
+            if (c + u < steps) step(uc, c + u);
+            landed(uc);
+        };
+        one(std::integral_constant<int, 0>{});
+        one(std::integral_constant<int, 1>{});
+        one(std::integral_constant<int, 2>{});
+        one(std::integral_constant<int, 3>{});
+    }
+    wait_vm<0>();                                          // nothing is on its way to LDS when the workgroup ends
+#pragma unroll
+    for (int b = 0; b < NBW; ++b) {
+        const int tb = 2 * b + wt;
+        if (tb >= nb) continue;
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            if (wf * 4 + a >= width) continue;
+            if (FIRST) store_hidden(g, acc[a][b], pb0 + tb, fb0 + wf * 4 + a);
+            else store_rows(g, acc[a][b], m0 + tb * 32 + (lane & 31), m0 + tb * 32 + (lane & 31) < seg_b, (fb0 + wf * 4 + a) * 32);
+        }
+    }
 }
 
 // ------------------------------------------------------------------ loads of experts
@@ -293,8 +545,20 @@ __global__ __launch_bounds__(256) void pack_mx_kernel(const uint16_t* __restrict
     }
 }
 
+template <bool FIRST, int TBK, int ST>
+int launch_tile(const MxArgs& g, hipStream_t s) {
+    const size_t tiles = (size_t)g.rows / (32 * TBK) + std::min(g.nslots, g.rows);   // an upper bound of the sum of ceil(len / (32 TBK))
+    const size_t wgs = (tiles * ((g.N / 32 + 7) / 8) + 7) / 8 * 8;
+    static smoe_lds_raised raised;
+    constexpr size_t lds = TileShape<TBK, ST>::LDS;
+    if (int rc = raised.ensure((const void*)tile_mx_kernel<FIRST, TBK, ST>, lds, (int)lds)) return rc;
+    hipLaunchKernelGGL((tile_mx_kernel<FIRST, TBK, ST>), dim3((unsigned)wgs), dim3(256), lds, s, g);
+    return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
+}
+
 template <bool FIRST>
 int launch_product(const MxArgs& g, hipStream_t s) {
+    if (smoe_mx_tiles(g.rows, g.nslots)) return launch_tile<FIRST, 4, 3>(g, s);
     constexpr int SPLIT = 4;
     const int nfb = g.N >> 5, per = 4 / SPLIT, ftiles = (nfb + per - 1) / per;
     const size_t tiles = (size_t)(g.rows / 32 + std::min(g.nslots, g.rows));   // an upper bound of the sum of ceil(len / 32)

@@ -110,7 +110,8 @@ int smoe_describe_ffn(const smoe_layer_t* L, int T, int fused, char* out, size_t
     if (!L || !out || n == 0) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: null argument");
     if (T < 1 || T > L->cfg.max_tokens) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: T=%d outside [1,%d]", T, L->cfg.max_tokens);
     if (L->cfg.dtype == SMOE_MXFP8) {
-        snprintf(out, n, "stream_mx_kernel<true, 4> | stream_mx_kernel<false, 4>");
+        snprintf(out, n, smoe_mx_tiles(T, L->cfg.K) ? "tile_mx_kernel<true, 4, 3> | tile_mx_kernel<false, 4, 3>"
+                                                    : "stream_mx_kernel<true, 4> | stream_mx_kernel<false, 4>");
         return SMOE_OK;
     }
     if (L->cfg.dtype != SMOE_BF16) return smoe_describe_ffn_f32(L, T, out, n);

@@ -121,6 +121,8 @@ inline __host__ __device__ int smoe_mx_groups(int r) { return (smoe_mx_steps(r) 
 inline __host__ __device__ size_t smoe_mx_row_bytes(int r) { return (size_t)smoe_mx_steps(r) * 2048; }
 inline __host__ __device__ size_t smoe_mx_row_scales(int r) { return (size_t)smoe_mx_groups(r) * 256; }
 inline size_t smoe_mx_matrix_bytes(int R, int N) { return (size_t)(N / 32) * (smoe_mx_row_bytes(R) + smoe_mx_row_scales(R)); }
+// Whether the products of `rows` sorted rows run on tiles staged through LDS, or stream the weights for 32 rows at a time.
+inline bool smoe_mx_tiles(int rows, int slots) { return rows > 64 * slots; }
 inline size_t smoe_mx_hidden_blocks(const smoe_config& c) { return (size_t)(c.max_tokens + 31) / 32 + c.K; }   // segments re-based to 32 rows
 inline size_t smoe_mx_hidden_bytes(const smoe_config& c) {
     return smoe_mx_hidden_blocks(c) * (smoe_mx_row_bytes(c.d_ff) + smoe_mx_row_scales(c.d_ff));
