@@ -8,8 +8,8 @@ namespace {
 constexpr int TOPK_MAX = 16, GROUPS_MAX = 16;
 
 // T tokens of k choices each: the layer's per-token buffers hold one entry per pair.
-int check_pairs(const smoe_layer* L, int T, int k, const char* who, bool need_full) {
-    if (int rc = smoe_check_hot(L, T, who, need_full)) return rc;
+int check_pairs(const smoe_layer* L, int T, int k, const char* who) {
+    if (int rc = smoe_check_hot(L, T, who, false)) return rc;
     if (k < 1 || k > TOPK_MAX) return smoe_fail(SMOE_EINVAL, "%s: k=%d outside [1,%d]", who, k, TOPK_MAX);
     if ((int64_t)T * k > L->cfg.max_tokens)
         return smoe_fail(SMOE_EINVAL, "%s: T * k = %lld pairs exceed max_tokens=%d", who, (long long)T * k, L->cfg.max_tokens);
@@ -41,7 +41,7 @@ int smoe_route_topk(smoe_layer_t* L, const smoe_topk_rule* rule, const float* bi
                     float* orig_gate, int32_t* slot, float* gate, float* xnorm, void* stream) {
     if (!rule) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: null rule");
     const smoe_topk_rule& r = *rule;
-    if (int rc = check_pairs(L, T, r.k, "smoe_route_topk", true)) return rc;
+    if (int rc = check_pairs(L, T, r.k, "smoe_route_topk")) return rc;
     const smoe_config& c = L->cfg;
     if (r.score != SMOE_SCORE_SOFTMAX && r.score != SMOE_SCORE_SIGMOID)
         return smoe_fail(SMOE_EINVAL, "smoe_route_topk: unknown score %d", r.score);
@@ -55,6 +55,7 @@ int smoe_route_topk(smoe_layer_t* L, const smoe_topk_rule* rule, const float* bi
         return smoe_fail(SMOE_EINVAL, "smoe_route_topk: k=%d exceeds the %d experts of the kept groups", r.k, c.E / r.groups * r.groups_kept);
     if (r.renorm != 0 && r.renorm != 1) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: renorm must be 0 or 1");
     if (!std::isfinite(r.scale)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: scale must be finite");
+    if (int rc = smoe_check_hot(L, T, "smoe_route_topk", true)) return rc;
     if (T == 0) return SMOE_OK;
     if (!x || !orig_expert || !orig_gate || !slot || !gate || !xnorm) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: null buffer");
     if (smoe_misaligned(x, 16)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: x must be 16-byte aligned");
@@ -76,7 +77,7 @@ int smoe_route_topk(smoe_layer_t* L, const smoe_topk_rule* rule, const float* bi
 
 int smoe_permute_topk(smoe_layer_t* L, const void* x, const int32_t* slot, int T, int k, void* x_perm, int32_t* perm, int32_t* inv_perm,
                       int32_t* offsets, void* stream) {
-    if (int rc = check_pairs(L, T, k, "smoe_permute_topk", false)) return rc;
+    if (int rc = check_pairs(L, T, k, "smoe_permute_topk")) return rc;
     if (!offsets) return smoe_fail(SMOE_EINVAL, "smoe_permute_topk: null offsets");
     if (T > 0 && (!slot || !perm || !inv_perm)) return smoe_fail(SMOE_EINVAL, "smoe_permute_topk: null buffer");
     if (T > 0 && x_perm && !x) return smoe_fail(SMOE_EINVAL, "smoe_permute_topk: x_perm without x");
@@ -87,9 +88,10 @@ int smoe_permute_topk(smoe_layer_t* L, const void* x, const int32_t* slot, int T
 
 int smoe_expert_ffn_mx(smoe_layer_t* L, const void* q, const void* q_scale, const int32_t* perm, int k, const int32_t* offsets, int T,
                        void* y_perm, void* stream) {
-    if (int rc = check_pairs(L, T, k, "smoe_expert_ffn_mx", true)) return rc;
+    if (int rc = check_pairs(L, T, k, "smoe_expert_ffn_mx")) return rc;
     if (L->cfg.dtype != SMOE_MXFP8) return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn_mx: only layers with 8-bit slots (SMOE_MXFP8)");
     if (!perm && k != 1) return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn_mx: without perm row r is token r, which takes k = 1");
+    if (int rc = smoe_check_hot(L, T, "smoe_expert_ffn_mx", true)) return rc;
     if (T == 0) return SMOE_OK;
     if (!q || !q_scale || !offsets || !y_perm) return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn_mx: null buffer");
     if (smoe_misaligned(q, 16) || smoe_misaligned(q_scale, 8) || smoe_misaligned(y_perm, 16))
@@ -101,7 +103,7 @@ int smoe_expert_ffn_mx(smoe_layer_t* L, const void* q, const void* q_scale, cons
 
 int smoe_combine_topk(smoe_layer_t* L, const void* y_perm, const int32_t* inv_perm, const float* gate, const void* residual, int T, int k,
                       void* out, void* stream) {
-    if (int rc = check_pairs(L, T, k, "smoe_combine_topk", false)) return rc;
+    if (int rc = check_pairs(L, T, k, "smoe_combine_topk")) return rc;
     if (T == 0) return SMOE_OK;
     if (!y_perm || !inv_perm || !gate || !out) return smoe_fail(SMOE_EINVAL, "smoe_combine_topk: null buffer");
     if (smoe_misaligned(y_perm, 16) || smoe_misaligned(out, 16) || smoe_misaligned(residual, 16))
