@@ -13,6 +13,7 @@
 //                      workgroup needs them), the token tile is staged through LDS.
 
 #include <algorithm>
+#include <climits>
 #include <cstdio>
 #include <string>
 #include <type_traits>
@@ -23,7 +24,6 @@
 namespace {
 
 typedef smoe_mx_acc f32x16;
-constexpr int MAX_SLOTS = 256;            // K <= E <= 256 by the C ABI
 
 struct MxArgs {
     const uint8_t* x;                     // first product: q [tokens, R]; second: hidden, operand order
@@ -35,58 +35,14 @@ struct MxArgs {
     size_t wstride;                       // bytes of a slot
     const int32_t* phys;
     const int32_t* offsets;
-    int nslots, rows, R, N;
+    int nslots, rows, R, N, cus;
+    bool past;                            // weights come from memory (smoe_weights_outgrow_cache)
     uint8_t* h;                           // first product's output, operand order
     uint8_t* hs;
     uint16_t* y;                          // second product's output [rows, N]
 };
 
-// Row tiles of all slots form one list in slot order; segments are re-based to multiples of 32 rows in the hidden activations.
-struct SlotMap {
-    int first[MAX_SLOTS + 1];             // row tiles before slot k
-    int pad[MAX_SLOTS];                   // 32-row blocks before slot k
-    int a[MAX_SLOTS], b[MAX_SLOTS];       // clamped segment bounds
-};
-
-// Called by every thread of the workgroup; ends with a barrier.
-__device__ __forceinline__ void build_slot_map(SlotMap& m, const int32_t* __restrict__ offsets, int nslots, int rows, int bt) {
-    if (threadIdx.x < 64) {
-        const int lane = threadIdx.x;
-        int tiles_before = 0, pad_before = 0;
-        for (int base = 0; base < nslots; base += 64) {
-            const int k = base + lane;
-            int a = 0, b = 0, tiles = 0, pad = 0;
-            if (k < nslots) {
-                a = min(max(offsets[k], 0), rows);             // clamps guard misuse
-                b = max(min(max(offsets[k + 1], 0), rows), a);
-                tiles = (b - a + bt - 1) / bt;
-                pad = (b - a + 31) >> 5;
-            }
-            const int tin = smoe_wave_incl_scan(tiles), pin = smoe_wave_incl_scan(pad);
-            if (k < nslots) {
-                m.first[k] = tiles_before + tin - tiles;
-                m.pad[k] = pad_before + pin - pad;
-                m.a[k] = a;
-                m.b[k] = b;
-            }
-            tiles_before += __builtin_amdgcn_readlane(tin, 63);
-            pad_before += __builtin_amdgcn_readlane(pin, 63);
-        }
-        if (lane == 0) m.first[nslots] = tiles_before;
-    }
-    __syncthreads();
-}
-
-// The last slot whose first row tile is <= mt (empty slots repeat the next one's).
-__device__ __forceinline__ int slot_of_tile(const SlotMap& m, int nslots, int mt) {
-    const int lane = threadIdx.x & 63;
-    int nle = 0;
-    for (int base = 0; base < nslots; base += 64) {
-        const int k = base + lane;
-        nle += __popcll(__ballot(k < nslots && m.first[k] <= mt));
-    }
-    return __builtin_amdgcn_readfirstlane(nle - 1);
-}
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 __device__ __forceinline__ int token_of_row(const MxArgs& g, int row) {
     if (!g.perm) return min(row, g.tokens - 1);
@@ -150,91 +106,140 @@ __device__ __forceinline__ uint32_t half_scales(uint2 v, int left) {
 }
 
 // ------------------------------------------------------------------ few rows a slot
-// One item = 32 rows of a slot x (4 / SPLIT) feature blocks; the SPLIT waves of a feature block take a share of the reduction
-// each and meet in LDS.
-template <bool FIRST, int SPLIT>
-__global__ __launch_bounds__(256) void stream_mx_kernel(const MxArgs g) {
-    __shared__ SlotMap m;
-    __shared__ float part[4][16][64];
-    build_slot_map(m, g.offsets, g.nslots, g.rows, 32);
-    constexpr int PER = 4 / SPLIT;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int nfb = g.N >> 5, ftiles = (nfb + PER - 1) / PER;
-    const int mt = blockIdx.x / ftiles, ft = blockIdx.x - mt * ftiles;
-    if (mt >= m.first[g.nslots]) return;
-    const int slot = slot_of_tile(m, g.nslots, mt);
-    const int within = mt - m.first[slot], m0 = m.a[slot] + 32 * within, m_end = m.b[slot], rb = m.pad[slot] + within;
-    const int fb = ft * PER + wave / SPLIT, part_of = wave % SPLIT;
-    const bool on = fb < nfb;
-    const int steps = smoe_mx_steps(g.R), blocks = g.R >> 5;
-    const int groups = smoe_mx_groups(g.R), gper = (groups + SPLIT - 1) / SPLIT;   // shares are whole groups of four steps
-    const int lo = min(part_of * gper * 4, steps), hi = min(lo + gper * 4, steps);
+// One item = 32 rows of a slot x one feature block; the NW waves of a workgroup take a share of the reduction each and meet in LDS.  A wave asks for
+// BATCH steps at a time, one batch ahead of the products.  NT: the weights come from memory, not from the Infinity Cache, and are kept out of the
+// caches (smoe_weights_outgrow_cache).
+template <bool NT>
+__device__ __forceinline__ uint4 load_weights(const uint4* p) { return NT ? smoe_load_stream(p) : *p; }
+
+template <bool FIRST, int NW, int BATCH, bool NT>
+__global__ __launch_bounds__(64 * NW) void stream_mx_kernel(const MxArgs g) {
+    __shared__ float part[NW > 1 ? NW - 1 : 1][16][64];
+    const int wave = uni(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int nfb = g.N >> 5, item = blockIdx.x / nfb, fb = blockIdx.x - item * nfb;
+    // the item's slot and rows, worked out by every wave for itself: 32-row tiles of all slots in slot order
+    int m0 = 0, m_end = 0, rb = 0, phys = -1;
+    for (int base = 0, before = 0; base < g.nslots; base += 64) {
+        const int k = base + lane;
+        int a = 0, b = 0, p = 0;
+        if (k < g.nslots) {
+            p = g.phys[k];
+            a = min(max(g.offsets[k], 0), g.rows);         // clamps guard misuse
+            b = max(min(max(g.offsets[k + 1], 0), g.rows), a);
+        }
+        const int n = (b - a + 31) >> 5, incl = smoe_wave_incl_scan(n), all = __builtin_amdgcn_readlane(incl, 63);
+        if (item < before + all) {                         // uniform: the slot is among these 64
+            const int l = __popcll(__ballot(before + incl <= item));   // slots that end in front of the item
+            const int within = item - before - __builtin_amdgcn_readlane(incl - n, l);
+            m0 = __builtin_amdgcn_readlane(a, l) + 32 * within;
+            m_end = __builtin_amdgcn_readlane(b, l);
+            phys = __builtin_amdgcn_readlane(p, l);
+            rb = item;
+            break;
+        }
+        before += all;
+    }
+    if (phys < 0) return;
+    const int steps = smoe_mx_steps(g.R), blocks = g.R >> 5, share = (steps + NW - 1) / NW;
+    const int lo = min(wave * share, steps), hi = min(lo + share, steps);
     f32x16 acc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    if (on && lo < hi) {
-        const uint8_t* wslot = g.w + (size_t)g.phys[slot] * g.wstride;
+    if (lo < hi) {
+        const uint8_t* wslot = g.w + (size_t)phys * g.wstride;
         const uint4* wp = (const uint4*)(wslot + (size_t)fb * smoe_mx_row_bytes(g.R)) + lane;
-        const uint32_t* wsp = (const uint32_t*)(wslot + (size_t)nfb * smoe_mx_row_bytes(g.R) + (size_t)fb * smoe_mx_row_scales(g.R)) + lane;
+        const uint8_t* wsp = wslot + (size_t)nfb * smoe_mx_row_bytes(g.R) + (size_t)fb * smoe_mx_row_scales(g.R) + lane * 4;
+        uint4 w[2][BATCH][2], x[2][BATCH][2];
+        uint32_t ws[2][BATCH], xs[2][BATCH];
+        auto ask_w = [&](auto sc, int s0) {                // past the share: its last step again, not multiplied
+            constexpr int z = decltype(sc)::value;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const int s = min(s0 + i, hi - 1);
+                w[z][i][0] = load_weights<NT>(wp + (size_t)s * 128);
+                w[z][i][1] = load_weights<NT>(wp + (size_t)s * 128 + 64);
+                ws[z][i] = wsp[(s >> 2) * 256 + (s & 3)];
+            }
+        };
+        ask_w(std::integral_constant<int, 0>{}, lo);       // on their way while the token of the row is looked up
         const uint8_t *xrow, *xsrow;
         if (FIRST) {
             const int t = token_of_row(g, min(m0 + (lane & 31), m_end - 1));
             xrow = g.x + (size_t)t * g.R + 16 * (lane >> 5);
-            xsrow = g.xs + (size_t)t * g.pitch;
+            xsrow = g.xs + (size_t)t * g.pitch + (lane >> 5);
         } else {
             xrow = g.x + (size_t)rb * smoe_mx_row_bytes(g.R) + lane * 16;
             xsrow = g.xs + (size_t)rb * smoe_mx_row_scales(g.R) + lane * 4;
         }
-        for (int s0 = lo; s0 < hi; s0 += 4) {
-            uint4 w[4][2], x[4][2];
+        auto ask_x = [&](auto sc, int s0) {
+            constexpr int z = decltype(sc)::value;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int s = min(s0 + i, steps - 1);
-                w[i][0] = smoe_load_stream(wp + (size_t)s * 128);
-                w[i][1] = smoe_load_stream(wp + (size_t)s * 128 + 64);
-                if (FIRST) {
-                    const bool second = s * 64 + 32 < g.R;         // the last step may be half a step
-                    x[i][0] = *(const uint4*)(xrow + s * 64);
-                    x[i][1] = *(const uint4*)(xrow + s * 64 + (second ? 32 : 0));
-                    if (!second) x[i][1] = make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < BATCH; ++i) {
+                const int s = min(s0 + i, hi - 1);
+                if (FIRST) {                               // the last step may be half a step: nothing behind it is used
+                    const bool second = s * 64 + 32 < g.R;
+                    x[z][i][0] = *(const uint4*)(xrow + s * 64);
+                    x[z][i][1] = *(const uint4*)(xrow + s * 64 + (second ? 32 : 0));
+                    if (!second) x[z][i][1] = make_uint4(0, 0, 0, 0);
+                    const uint32_t v = xsrow[s * 2];
+                    xs[z][i] = 2 * s + (lane >> 5) < blocks ? v : 0;
                 } else {
-                    x[i][0] = *(const uint4*)(xrow + (size_t)s * 2048);
-                    x[i][1] = *(const uint4*)(xrow + (size_t)s * 2048 + 1024);
+                    x[z][i][0] = *(const uint4*)(xrow + (size_t)s * 2048);
+                    x[z][i][1] = *(const uint4*)(xrow + (size_t)s * 2048 + 1024);
+                    xs[z][i] = xsrow[(s >> 2) * 256 + (s & 3)];
                 }
             }
-            const uint32_t ws = wsp[(s0 >> 2) * 64];
-            const uint32_t xs = FIRST ? half_scales(*(const uint2*)(xsrow + (s0 >> 2) * 8), blocks - (s0 >> 2) * 8) : *(const uint32_t*)(xsrow + (s0 >> 2) * 256);
-            smoe_mx_mfma<0>(acc, w[0], x[0], ws, xs);
-            if (s0 + 1 < hi) smoe_mx_mfma<1>(acc, w[1], x[1], ws, xs);
-            if (s0 + 2 < hi) smoe_mx_mfma<2>(acc, w[2], x[2], ws, xs);
-            if (s0 + 3 < hi) smoe_mx_mfma<3>(acc, w[3], x[3], ws, xs);
+        };
+        auto multiply = [&](auto sc, int s0) {
+            constexpr int z = decltype(sc)::value;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (s0 + i < hi) smoe_mx_mfma<0>(acc, w[z][i], x[z][i], ws[z][i], xs[z][i]);
+        };
+        ask_x(std::integral_constant<int, 0>{}, lo);
+        for (int s0 = lo; s0 < hi; s0 += 2 * BATCH) {
+            if (s0 + BATCH < hi) {
+                ask_w(std::integral_constant<int, 1>{}, s0 + BATCH);
+                ask_x(std::integral_constant<int, 1>{}, s0 + BATCH);
+            }
+            __builtin_amdgcn_sched_barrier(0);             // the next batch is on its way
+            multiply(std::integral_constant<int, 0>{}, s0);
+            if (s0 + BATCH >= hi) break;
+            if (s0 + 2 * BATCH < hi) {
+                ask_w(std::integral_constant<int, 0>{}, s0 + 2 * BATCH);
+                ask_x(std::integral_constant<int, 0>{}, s0 + 2 * BATCH);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(std::integral_constant<int, 1>{}, s0 + BATCH);
         }
     }
-    if (SPLIT > 1) {
-        if (part_of)
+    if (wave)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[wave][i][lane] = acc[i];
-        __syncthreads();
-        if (part_of) return;
+        for (int i = 0; i < 16; ++i) part[wave - 1][i][lane] = acc[i];
+    __syncthreads();
+    if (wave) return;
 #pragma unroll
-        for (int q = 1; q < SPLIT; ++q)                        // in order of the reduction
+    for (int q = 0; q < NW - 1; ++q)                       // in order of the reduction
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] += part[wave + q][i][lane];
-    }
-    if (!on) return;
+        for (int i = 0; i < 16; ++i) acc[i] += part[q][i][lane];
     if (FIRST) store_hidden(g, acc, rb, fb);
     else store_rows(g, acc, m0 + (lane & 31), m0 + (lane & 31) < m_end, fb * 32);
 }
 
 // ------------------------------------------------------------------ many rows a slot
-// Tile = at most 256 features (8 blocks of 32) x at most 32 * TBK tokens, both operands staged through a ring of ST stages in LDS, one step of 64
-// reduction elements a stage.  Four waves: wave (wf, wt) multiplies four feature blocks with the token blocks of parity wt.  Loads go from
-// memory to LDS without passing through registers, ST - 1 steps ahead; each wave issues the same number of them a step, so that one count says
-// what has landed.  The scales of four steps come the same way, in front of the first step's operands.
+// Tile = FB blocks of 32 features x at most TBK blocks of 32 tokens, both operands staged through a ring of ST stages in LDS, one step of 64 reduction
+// elements a stage.  Four waves, WF along the features and WT along the tokens.  Loads go from memory to LDS without passing through registers,
+// ST - 1 steps ahead; each wave issues the same number of them a step, so that one count says what has landed.  The scales of four steps
+// come the same way, in front of the first step's operands.
+//
+// Two workgroups to a compute unit (FB = 8: 80 KB of LDS each), so that one multiplies while the other waits at its barrier, looks its next tile up
+// or narrows its results.  A workgroup of 256 x 256 tiles with twice the accumulators moves a third fewer bytes a product, but its waves are alone on
+// their SIMDs: 239 us for the 16384 rows of 1024 x 4096 that take 190 here, 210 with its next tile's loads in flight through the stores.  Traces of copies
+// without a part (one slot, first + second product, 171 us): without loads 140, without products 143, without stores 133.
 extern __shared__ __align__(16) char mx_lds[];
 constexpr int MX_BLK = 2048;              // bytes of a block of one step
+constexpr int TILE_COST0 = 20;            // a tile beside its steps, in steps of one token block; 0 to 60 chose tiles of the same speed
 
-__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ uint32_t lds_addr(uint32_t off) {
     return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(mx_lds + off);
 }
@@ -257,59 +262,72 @@ __device__ __forceinline__ void wait_vm() {   // at most the N youngest vector m
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int TBK, int ST>
+// Multiples of four in [lo, hi).
+constexpr int group_starts(int lo, int hi) { return (hi + 3) / 4 - (lo + 3) / 4; }
+
+constexpr int TBK = 4;                    // most token blocks of a tile
+template <int FB, int ST>
 struct TileShape {
-    static constexpr uint32_t STAGE = (8 + TBK) * MX_BLK;
-    static constexpr uint32_t SC = ST * STAGE;             // scales of two groups: weights [8][256], tokens [TBK][256]
-    static constexpr uint32_t SCG = (8 + TBK) * 256;
+    static constexpr uint32_t STAGE = (FB + TBK) * MX_BLK;
+    static constexpr uint32_t SC = ST * STAGE;             // scales of two groups: weights [FB][256], tokens [TBK][256]
+    static constexpr uint32_t SCG = (FB + TBK) * 256;
     static constexpr size_t LDS = SC + 2 * SCG;
 };
 
-template <bool FIRST, int TBK, int ST>
-__global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const MxArgs g) {
-    using S = TileShape<TBK, ST>;
-    constexpr int TW = TBK / 4;                            // token blocks that a wave loads
-    constexpr int NBW = TBK / 2;                           // token blocks that a wave multiplies
-    constexpr int PER = 4 + 2 * TW, NSC = FIRST ? 1 + TW : 2;   // loads of a wave a step, and of the scales a group
+template <bool FIRST, int FB, int ST>
+__global__ __launch_bounds__(256, FB == 8 ? 2 : 3) void tile_mx_kernel(const MxArgs g) {
+    using S = TileShape<FB, ST>;
+    constexpr int WF = FB == 2 ? 1 : 2, WT = 4 / WF;       // waves along the features and along the tokens
+    constexpr int AW = FB / WF, NBW = TBK / WT;            // feature and token blocks that a wave multiplies
+    constexpr int WL = FB / 4;                             // feature blocks that a wave loads (0: half a block)
+    constexpr int PER = (FB == 2 ? 1 : 2 * WL) + 2, NSC = 2;    // its loads a step, and of the scales a group
     const int tid = threadIdx.x, wave = uni(tid >> 6), lane = tid & 63;
-    const int wf = wave & 1, wt = wave >> 1;
-    const int nfb = g.N >> 5, ftiles = (nfb + 7) >> 3;
+    const int wf = wave % WF, wt = wave / WF;
+    const int nfb = g.N >> 5, ftiles = (nfb + FB - 1) / FB, steps = smoe_mx_steps(g.R);
     // This workgroup's item.  Row tiles of all slots in slot order; inside a slot the row tile fastest (first product) or the feature tile.  The
     // dies take an eighth of the list each (workgroups are dealt to them in turn), so that few slots' weights pass through an L2.
-    int tiles_all = 0;
-    for (int base = 0; base < g.nslots; base += 64) {
-        const int k = base + lane;
-        int len = 0;
+    int seg_a, seg_b;                                      // of slot `lane`
+    auto segment = [&](int k, int& a, int& b) {
+        a = b = 0;
         if (k < g.nslots) {
-            const int a = min(max(g.offsets[k], 0), g.rows);
-            len = max(min(max(g.offsets[k + 1], 0), g.rows), a) - a;
+            a = min(max(g.offsets[k], 0), g.rows);         // clamps guard misuse
+            b = max(min(max(g.offsets[k + 1], 0), g.rows), a);
         }
-        tiles_all += __builtin_amdgcn_readlane(smoe_wave_incl_scan(((len + 31) / 32 + TBK - 1) / TBK), 63);
+    };
+    segment(lane, seg_a, seg_b);
+    // Height of the row tiles: those of at most 1, 2, .. blocks are counted, all take the best.
+    int H = TBK, G = 0, best = INT_MAX;
+#pragma unroll
+    for (int h = TBK; h >= 1; --h) {
+        int n = 0;
+        for (int base = 0; base < g.nslots; base += 64) {
+            int a = seg_a, b = seg_b;
+            if (base) segment(base + lane, a, b);
+            n += __builtin_amdgcn_readlane(smoe_wave_incl_scan((((b - a + 31) >> 5) + h - 1) / h), 63);
+        }
+        const int cost = ((n * ftiles + g.cus - 1) / g.cus) * (steps * (1 + h) + TILE_COST0);
+        if (cost < best) { best = cost; H = h; G = n * ftiles; }
     }
-    const int G = tiles_all * ftiles, die = blockIdx.x % 8;
-    const int lo = (int)((long long)G * die / 8), hi = (int)((long long)G * (die + 1) / 8), item = lo + blockIdx.x / 8;
-    if (item >= hi) return;
-    int slot = 0, seg_a = 0, seg_b = 0, first = 0, pad = 0, tiles = 1;
+    const int die = blockIdx.x % 8;
+    const int lo = (int)((long long)G * die / 8), hi = (int)((long long)G * (die + 1) / 8);
+    for (int item = lo + blockIdx.x / 8; item < hi; item += gridDim.x / 8) {
+    int slot = 0, slot_a = 0, slot_b = 0, first = 0, pad = 0, tiles = 1;
     {
         int before = 0, pad_before = 0;
         for (int base = 0; base < g.nslots; base += 64) {
-            const int k = base + lane;
-            int a = 0, b = 0;
-            if (k < g.nslots) {
-                a = min(max(g.offsets[k], 0), g.rows);
-                b = max(min(max(g.offsets[k + 1], 0), g.rows), a);
-            }
-            const int blocks = (b - a + 31) >> 5, n = (blocks + TBK - 1) / TBK;
-            const int incl = smoe_wave_incl_scan(n), pincl = smoe_wave_incl_scan(blocks);
+            int a = seg_a, b = seg_b;
+            if (base) segment(base + lane, a, b);
+            const int nblk = (b - a + 31) >> 5, n = (nblk + H - 1) / H;
+            const int incl = smoe_wave_incl_scan(n), pincl = smoe_wave_incl_scan(nblk);
             const int all = __builtin_amdgcn_readlane(incl, 63);
             if (item < (before + all) * ftiles) {          // uniform: the slot is among these 64
                 const int l = __popcll(__ballot((before + incl) * ftiles <= item));   // slots that end in front of the item
                 slot = base + l;
-                seg_a = __builtin_amdgcn_readlane(a, l);
-                seg_b = __builtin_amdgcn_readlane(b, l);
+                slot_a = __builtin_amdgcn_readlane(a, l);
+                slot_b = __builtin_amdgcn_readlane(b, l);
                 tiles = __builtin_amdgcn_readlane(n, l);
                 first = before + __builtin_amdgcn_readlane(incl, l) - tiles;
-                pad = pad_before + __builtin_amdgcn_readlane(pincl - blocks, l);
+                pad = pad_before + __builtin_amdgcn_readlane(pincl - nblk, l);
                 break;
             }
             before += all;
@@ -318,91 +336,89 @@ __global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const Mx
     }
     const int local = item - first * ftiles;
     const int ft = FIRST ? local / tiles : local % ftiles, rt = FIRST ? local % tiles : local / ftiles;
-    const int nbk = (seg_b - seg_a + 31) >> 5, bq = nbk / tiles, br = nbk - bq * tiles;     // rows and features are cut evenly
+    const int nbk = (slot_b - slot_a + 31) >> 5, bq = nbk / tiles, br = nbk - bq * tiles;     // rows and features are cut evenly
     const int b0 = rt * bq + min(rt, br), nb = bq + (rt < br ? 1 : 0);
-    const int m0 = seg_a + 32 * b0, pb0 = pad + b0;
+    const int m0 = slot_a + 32 * b0, pb0 = pad + b0;
     const int fq = nfb / ftiles, fr = nfb - fq * ftiles, fb0 = ft * fq + min(ft, fr), width = fq + (ft < fr ? 1 : 0);
-    const int steps = smoe_mx_steps(g.R), blocks = g.R >> 5;
+    const int blocks = g.R >> 5;
 
     // load side
     const char* wslot = (const char*)g.w + (size_t)g.phys[slot] * g.wstride;
     const size_t rowb = smoe_mx_row_bytes(g.R), rows_ = smoe_mx_row_scales(g.R);
     const uint32_t lane16 = lane * 16;
-    const char* wsrc[2];
-    uint64_t wlanes[2];
+    constexpr int WN = WL ? WL : 1;
+    const char* wsrc[WN];
+    uint64_t wlanes[WN];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int f = 2 * wave + i;
+    for (int i = 0; i < WN; ++i) {
+        const int f = FB == 2 ? wave >> 1 : WL * wave + i;
         wlanes[i] = f < width ? ~0ull : 1;                 // a block that is not there: one lane's load, so that the counts stay
         wsrc[i] = wslot + (size_t)(fb0 + min(f, width - 1)) * rowb;
     }
-    const char* wscale = wslot + (size_t)nfb * rowb + (size_t)(fb0 + min(2 * wave + ((lane >> 4) & 1), width - 1)) * rows_ + (lane & 15) * 16;
-    const char *tsrc[TW][2], *tscale[TW];                  // FIRST: this lane's two rows; else scalar bases (tsrc[.][0])
-    uint64_t tlanes[TW];
+    const int sblk = FB == 8 ? 2 * wave + ((lane >> 4) & 1) : wave % FB;      // scales: 16 lanes a block
+    const char* wscale = wslot + (size_t)nfb * rowb + (size_t)(fb0 + min(sblk, width - 1)) * rows_ + (lane & 15) * 16;
+    const int unit = (lane & 3) ^ ((lane >> 3) & 3);       // rows of 64 bytes whose four units are permuted by (row / 2) % 4: operand reads of
+                                                           // neighbouring lanes hit all banks
+    const char *tsrc[2], *tscale = nullptr;                // FIRST: this lane's two rows of block `wave`; else a scalar base (tsrc[0])
+    const uint64_t tlanes = wave < nb ? ~0ull : 1;
+    const int bc = min(wave, nb - 1);
+    if (FIRST) {
 #pragma unroll
-    for (int i = 0; i < TW; ++i) {
-        const int b = TW * wave + i;
-        tlanes[i] = b < nb ? ~0ull : 1;
-        const int bc = min(b, nb - 1);
-        if (FIRST) {
-            // rows of 64 bytes whose four units are permuted by (row / 2) % 4: operand reads of neighbouring lanes hit all banks
-            const uint32_t u = (lane & 3) ^ ((lane >> 3) & 3);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t = token_of_row(g, min(m0 + bc * 32 + h * 16 + (lane >> 2), seg_b - 1));
-                tsrc[i][h] = (const char*)g.x + (size_t)t * g.R + u * 16;
-            }
-            const int t = token_of_row(g, min(m0 + bc * 32 + (lane & 31), seg_b - 1));
-            tscale[i] = (const char*)g.xs + (size_t)t * g.pitch + (lane >> 5) * 4;
-        } else {
-            tsrc[i][0] = (const char*)g.x + (size_t)(pb0 + bc) * rowb;
-            tscale[i] = nullptr;
+        for (int h = 0; h < 2; ++h) {
+            const int t = token_of_row(g, min(m0 + bc * 32 + h * 16 + (lane >> 2), slot_b - 1));
+            tsrc[h] = (const char*)g.x + (size_t)t * g.R + unit * 16;
         }
+        const int t = token_of_row(g, min(m0 + bc * 32 + (lane & 31), slot_b - 1));
+        tscale = (const char*)g.xs + (size_t)t * g.pitch + (lane >> 5) * 4;
+    } else {
+        tsrc[0] = (const char*)g.x + (size_t)(pb0 + bc) * rowb;
+        tscale = (const char*)g.xs + (size_t)(pb0 + bc) * rows_ + (lane & 15) * 16;
     }
-    const char* hscale = FIRST ? nullptr : (const char*)g.xs + (size_t)(pb0 + min(TW * wave + (lane >> 4) % TW, nb - 1)) * rows_ + (lane & 15) * 16;
     uint32_t lst = 0;
     auto issue = [&](int c) {                              // loads of step c into stage lst; past the last: one lane's, nowhere read
         const bool in = c < steps;
         if ((c & 3) == 0) {
             const uint32_t sc = S::SC + ((c >> 2) & 1) * S::SCG;
             const int gr = min(c >> 2, smoe_mx_groups(g.R) - 1);
-            dma_16(wscale + (size_t)gr * 256, sc + wave * 512, 0xffffffffull);
-            if (FIRST) {
+            dma_16(wscale + (size_t)gr * 256, sc + (FB == 8 ? wave * 512 : wave % FB * 256), FB == 8 ? 0xffffffffull : 0xffffull);
+            if (FIRST) dma_4(tscale + gr * 8, sc + FB * 256 + wave * 256);
+            else dma_16(tscale + (size_t)gr * 256, sc + FB * 256 + wave * 256, 0xffffull);
+        }
+        const bool on = c + 1 < steps;                     // the next step's place
+        if constexpr (FB == 2) {
+            dma_16(wsrc[0] + (wave & 1) * 1024 + lane16, lst + wave * 1024, in ? wlanes[0] : 1);
+            wsrc[0] += on ? MX_BLK : 0;
+        } else {
 #pragma unroll
-                for (int i = 0; i < TW; ++i) dma_4(tscale[i] + gr * 8, sc + 2048 + (TW * wave + i) * 256);
-            } else {
-                dma_16(hscale + (size_t)gr * 256, sc + 2048 + wave * TW * 256, TW == 1 ? 0xffffull : 0xffffffffull);
+            for (int i = 0; i < WL; ++i) {
+                dma_2k(wsrc[i], lane16, lst + (WL * wave + i) * MX_BLK, in ? wlanes[i] : 1);
+                wsrc[i] += on ? MX_BLK : 0;
             }
         }
-        const int cc = in ? c : steps - 1;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            dma_2k(wsrc[i] + (size_t)cc * MX_BLK, lane16, lst + (2 * wave + i) * MX_BLK, in ? wlanes[i] : 1);
-#pragma unroll
-        for (int i = 0; i < TW; ++i) {
-            const uint32_t at = lst + (8 + TW * wave + i) * MX_BLK;
-            if (FIRST) {
-                // a row that ends in the middle of the step: its last 32 bytes again, which meet zeros
-                const int u = (lane & 3) ^ ((lane >> 3) & 3);
-                const int back = cc * 64 + 32 >= g.R && u >= 2 ? 32 : 0;
-                dma_16(tsrc[i][0] + cc * 64 - back, at, in ? tlanes[i] : 1);
-                dma_16(tsrc[i][1] + cc * 64 - back, at + 1024, in ? tlanes[i] : 1);
-            } else {
-                dma_2k(tsrc[i][0] + (size_t)cc * MX_BLK, lane16, at, in ? tlanes[i] : 1);
-            }
+        const uint32_t at = lst + (FB + wave) * MX_BLK;
+        if (FIRST) {
+            // a row that ends in the middle of the last step: its last 32 bytes again, which meet zeros
+            const int back = c == steps - 1 && (g.R & 32) && unit >= 2 ? 32 : 0;
+            dma_16(tsrc[0] - back, at, in ? tlanes : 1);
+            dma_16(tsrc[1] - back, at + 1024, in ? tlanes : 1);
+            tsrc[0] += on ? 64 : 0;
+            tsrc[1] += on ? 64 : 0;
+        } else {
+            dma_2k(tsrc[0], lane16, at, in ? tlanes : 1);
+            tsrc[0] += on ? MX_BLK : 0;
         }
         lst = lst == (ST - 1) * S::STAGE ? 0 : lst + S::STAGE;
     };
 
-    f32x16 acc[4][NBW];
+    f32x16 acc[AW][NBW];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < AW; ++a)
 #pragma unroll
         for (int b = 0; b < NBW; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
     uint32_t cst = 0;
-    uint32_t ws[4], ts[NBW];
+    uint32_t ws[AW], ts[NBW];
     const uint32_t toff0 = FIRST ? (lane & 31) * 64 + (((lane >> 5) ^ ((lane >> 1) & 3)) * 16) : lane16;
     const uint32_t toff1 = FIRST ? (lane & 31) * 64 + (((2 + (lane >> 5)) ^ ((lane >> 1) & 3)) * 16) : lane16 + 1024;
     auto step = [&](auto uc, int c) {
@@ -410,10 +426,10 @@ __global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const Mx
         if (u == 0) {
             const uint32_t sc = S::SC + ((c >> 2) & 1) * S::SCG;
 #pragma unroll
-            for (int a = 0; a < 4; ++a) ws[a] = *(const uint32_t*)(mx_lds + sc + (wf * 4 + a) * 256 + lane * 4);
+            for (int a = 0; a < AW; ++a) ws[a] = *(const uint32_t*)(mx_lds + sc + (wf * AW + a) * 256 + lane * 4);
 #pragma unroll
             for (int b = 0; b < NBW; ++b) {
-                const char* p = mx_lds + sc + 2048 + (2 * b + wt) * 256;
+                const char* p = mx_lds + sc + FB * 256 + (b * WT + wt) * 256;
                 if (FIRST) {
                     const uint32_t x = *(const uint32_t*)(p + (lane & 31) * 4), y = *(const uint32_t*)(p + 128 + (lane & 31) * 4);
                     ts[b] = half_scales(make_uint2(x, y), blocks - (c >> 2) * 8);
@@ -422,29 +438,30 @@ __global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const Mx
                 }
             }
         }
-        uint4 wv[4][2], tv[NBW][2];
+        uint4 wv[AW][2], tv[NBW][2];
 #pragma unroll
         for (int b = 0; b < NBW; ++b) {
-            const char* p = mx_lds + cst + (8 + 2 * b + wt) * MX_BLK;
+            const char* p = mx_lds + cst + (FB + b * WT + wt) * MX_BLK;
             tv[b][0] = *(const uint4*)(p + toff0);
             tv[b][1] = *(const uint4*)(p + toff1);
         }
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const char* p = mx_lds + cst + (wf * 4 + a) * MX_BLK + lane16;
+        for (int a = 0; a < AW; ++a) {
+            const char* p = mx_lds + cst + (wf * AW + a) * MX_BLK + lane16;
             wv[a][0] = *(const uint4*)p;
             wv[a][1] = *(const uint4*)(p + 1024);
         }
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
+        for (int a = 0; a < AW; ++a)
 #pragma unroll
-            for (int b = 0; b < NBW; ++b) smoe_mx_mfma<u>(acc[a][b], wv[a], tv[b], ws[a], ts[b]);
+            for (int b = 0; b < NBW; ++b)
+                if (b == 0 || b * WT + wt < nb) smoe_mx_mfma<u>(acc[a][b], wv[a], tv[b], ws[a], ts[b]);
         cst = cst == (ST - 1) * S::STAGE ? 0 : cst + S::STAGE;
     };
     // Step c + 1 has landed: what may be outstanding are the loads of the ST - 2 steps behind it.
     auto landed = [&](auto uc) {
         constexpr int u = decltype(uc)::value;
-        constexpr int younger = (ST - 2) * PER + ((u + 2) % 4 == 0 || (ST > 3 && (u + 3) % 4 == 0) ? NSC : 0);
+        constexpr int younger = (ST - 2) * PER + group_starts(u + 2, u + ST) * NSC;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // this wave's reads of the stage that is loaded next are done
         wait_vm<younger>();
         __builtin_amdgcn_s_barrier();
@@ -465,17 +482,19 @@ __global__ __launch_bounds__(256, TBK == 4 ? 2 : 1) void tile_mx_kernel(const Mx
         one(std::integral_constant<int, 2>{});
         one(std::integral_constant<int, 3>{});
     }
-    wait_vm<0>();                                          // nothing is on its way to LDS when the workgroup ends
+    wait_vm<0>();                                          // nothing is on its way to LDS when the next tile's loads, or the workgroup's end, come
+    __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int b = 0; b < NBW; ++b) {
-        const int tb = 2 * b + wt;
+        const int tb = b * WT + wt;
         if (tb >= nb) continue;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            if (wf * 4 + a >= width) continue;
-            if (FIRST) store_hidden(g, acc[a][b], pb0 + tb, fb0 + wf * 4 + a);
-            else store_rows(g, acc[a][b], m0 + tb * 32 + (lane & 31), m0 + tb * 32 + (lane & 31) < seg_b, (fb0 + wf * 4 + a) * 32);
+        for (int a = 0; a < AW; ++a) {
+            if (wf * AW + a >= width) continue;
+            if (FIRST) store_hidden(g, acc[a][b], pb0 + tb, fb0 + wf * AW + a);
+            else store_rows(g, acc[a][b], m0 + tb * 32 + (lane & 31), m0 + tb * 32 + (lane & 31) < slot_b, (fb0 + wf * AW + a) * 32);
         }
+    }
     }
 }
 
@@ -545,25 +564,40 @@ __global__ __launch_bounds__(256) void pack_mx_kernel(const uint16_t* __restrict
     }
 }
 
-template <bool FIRST, int TBK, int ST>
+template <bool FIRST, int NW, int BATCH, bool NT>
+int launch_stream_as(const MxArgs& g, hipStream_t s) {
+    const size_t tiles = (size_t)(g.rows / 32 + std::min(g.nslots, g.rows));   // an upper bound of the sum of ceil(len / 32)
+    hipLaunchKernelGGL((stream_mx_kernel<FIRST, NW, BATCH, NT>), dim3((unsigned)(tiles * (g.N / 32))), dim3(64 * NW), 0, s, g);
+    return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
+}
+
+template <bool FIRST>
+int launch_stream(const MxArgs& g, hipStream_t s) {
+    // Two waves to a feature block, of two steps a batch, for short reductions; four, of four steps, from 25 steps on, where a wave has more to ask for.
+    // (us; 10 slots of 768 x 3072, 13 tokens: first product 7.4 with four steps a batch, 6.8 with two, 7.8 with four waves, and 13.8 with eight of four
+    // steps; second product 7.0 with four waves of four steps, 7.2 of two, 8.0 with two waves, 7.7 with eight; 16 slots, 32 tokens: 12.5, 10.3, 12.3 and 21.8;
+    // 10.5, 12.9, 10.2 and 13.2)
+    if (smoe_mx_steps(g.R) <= 24) return g.past ? launch_stream_as<FIRST, 2, 2, true>(g, s) : launch_stream_as<FIRST, 2, 2, false>(g, s);
+    return g.past ? launch_stream_as<FIRST, 4, 4, true>(g, s) : launch_stream_as<FIRST, 4, 4, false>(g, s);
+}
+
+template <bool FIRST, int FB, int ST>
 int launch_tile(const MxArgs& g, hipStream_t s) {
-    const size_t tiles = (size_t)g.rows / (32 * TBK) + std::min(g.nslots, g.rows);   // an upper bound of the sum of ceil(len / (32 TBK))
-    const size_t wgs = (tiles * ((g.N / 32 + 7) / 8) + 7) / 8 * 8;
     static smoe_lds_raised raised;
-    constexpr size_t lds = TileShape<TBK, ST>::LDS;
-    if (int rc = raised.ensure((const void*)tile_mx_kernel<FIRST, TBK, ST>, lds, (int)lds)) return rc;
-    hipLaunchKernelGGL((tile_mx_kernel<FIRST, TBK, ST>), dim3((unsigned)wgs), dim3(256), lds, s, g);
+    constexpr size_t lds = TileShape<FB, ST>::LDS;
+    if (int rc = raised.ensure((const void*)tile_mx_kernel<FIRST, FB, ST>, lds, (int)lds)) return rc;
+    hipLaunchKernelGGL((tile_mx_kernel<FIRST, FB, ST>), dim3(2 * g.cus), dim3(256), lds, s, g);
     return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
 }
 
 template <bool FIRST>
 int launch_product(const MxArgs& g, hipStream_t s) {
-    if (smoe_mx_tiles(g.rows, g.nslots)) return launch_tile<FIRST, 4, 3>(g, s);
-    constexpr int SPLIT = 4;
-    const int nfb = g.N >> 5, per = 4 / SPLIT, ftiles = (nfb + per - 1) / per;
-    const size_t tiles = (size_t)(g.rows / 32 + std::min(g.nslots, g.rows));   // an upper bound of the sum of ceil(len / 32)
-    hipLaunchKernelGGL((stream_mx_kernel<FIRST, SPLIT>), dim3((unsigned)(tiles * ftiles)), dim3(256), 0, s, g);
-    return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
+    switch (smoe_mx_form(g.rows, g.nslots, g.N)) {
+        case 8: return launch_tile<FIRST, 8, 3>(g, s);
+        case 4: return launch_tile<FIRST, 4, 3>(g, s);
+        case 2: return launch_tile<FIRST, 2, 4>(g, s);
+    }
+    return launch_stream<FIRST>(g, s);
 }
 
 }  // namespace
@@ -606,6 +640,8 @@ int smoe_launch_ffn_mx(const smoe_layer* L, const void* q, const void* q_scale, 
     g.h = h;
     g.hs = hs;
     g.y = (uint16_t*)y_perm;
+    g.cus = 256;
+    g.past = smoe_weights_outgrow_cache(L);
     int rc = launch_product<true>(g, s);
     if (rc) return rc;
     g.x = h;

@@ -110,8 +110,17 @@ int smoe_describe_ffn(const smoe_layer_t* L, int T, int fused, char* out, size_t
     if (!L || !out || n == 0) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: null argument");
     if (T < 1 || T > L->cfg.max_tokens) return smoe_fail(SMOE_EINVAL, "smoe_describe_ffn: T=%d outside [1,%d]", T, L->cfg.max_tokens);
     if (L->cfg.dtype == SMOE_MXFP8) {
-        snprintf(out, n, smoe_mx_tiles(T, L->cfg.K) ? "tile_mx_kernel<true, 4, 3> | tile_mx_kernel<false, 4, 3>"
-                                                    : "stream_mx_kernel<true, 4> | stream_mx_kernel<false, 4>");
+        char name[2][48];
+        for (int i = 0; i < 2; ++i) {
+            const int form = smoe_mx_form(T, L->cfg.K, i ? L->cfg.d_model : L->cfg.d_ff);
+            const char* first = i ? "false" : "true";
+            if (form) snprintf(name[i], sizeof(name[i]), "tile_mx_kernel<%s, %d, %d>", first, form, form == 2 ? 4 : 3);
+            else {
+                const int nw = smoe_mx_steps(i ? L->cfg.d_ff : L->cfg.d_model) <= 24 ? 2 : 4;
+                snprintf(name[i], sizeof(name[i]), "stream_mx_kernel<%s, %d, %d, %s>", first, nw, nw, smoe_weights_outgrow_cache(L) ? "true" : "false");
+            }
+        }
+        snprintf(out, n, "%s | %s", name[0], name[1]);
         return SMOE_OK;
     }
     if (L->cfg.dtype != SMOE_BF16) return smoe_describe_ffn_f32(L, T, out, n);

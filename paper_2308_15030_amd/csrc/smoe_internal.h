@@ -121,8 +121,17 @@ inline __host__ __device__ int smoe_mx_groups(int r) { return (smoe_mx_steps(r) 
 inline __host__ __device__ size_t smoe_mx_row_bytes(int r) { return (size_t)smoe_mx_steps(r) * 2048; }
 inline __host__ __device__ size_t smoe_mx_row_scales(int r) { return (size_t)smoe_mx_groups(r) * 256; }
 inline size_t smoe_mx_matrix_bytes(int R, int N) { return (size_t)(N / 32) * (smoe_mx_row_bytes(R) + smoe_mx_row_scales(R)); }
-// Whether the products of `rows` sorted rows run on tiles staged through LDS, or stream the weights for 32 rows at a time.
-inline bool smoe_mx_tiles(int rows, int slots) { return rows > 64 * slots; }
+// Form of a product with N features on `rows` sorted rows (ffn_mx.hip): feature blocks of its tiles, 8, 4 or 2, or 0 where the weights are
+// streamed for 32 rows at a time.  Up to 32 rows a slot nothing but the weights counts.  Beyond, the widest tile that still gives most of
+// the 256 compute units one; the reduction of a single tile is a chain of steps, so narrower ones, with less to do a step, end earlier where there
+// are few.  Measured (us, 8 / 4 / 2 / streamed; tiles of 8 blocks): 16384 rows, 32 slots, 1024 -> 4096 (2304 tiles) 115 / 146 / 209 / 443; 4000 rows, 4096 -> 1024
+// (188) 45 / 49 / 51 / 93; 2400 rows, 8 slots, 2048 -> 768 (69) 17 / 12 / 14 / 21; 2426 rows, 11 slots, 1696 -> 416 (48) 14 / 11 / 9 / 17; 600 rows,
+// 4 slots, 3072 -> 768 (21) 21 / 15 / 14 / 10; 128 rows, 16 slots, 3072 -> 768 23 / 20 / 15 / 13.
+inline int smoe_mx_form(int rows, int slots, int N) {
+    if (rows <= 32 * slots) return 0;
+    const int tiles = (rows / 128 + (slots + 1) / 2) * ((N / 32 + 7) / 8);      // half a row tile more a slot, for its end
+    return tiles < 24 ? 0 : tiles < 56 ? 2 : tiles < 184 ? 4 : 8;
+}
 inline size_t smoe_mx_hidden_blocks(const smoe_config& c) { return (size_t)(c.max_tokens + 31) / 32 + c.K; }   // segments re-based to 32 rows
 inline size_t smoe_mx_hidden_bytes(const smoe_config& c) {
     return smoe_mx_hidden_blocks(c) * (smoe_mx_row_bytes(c.d_ff) + smoe_mx_row_scales(c.d_ff));

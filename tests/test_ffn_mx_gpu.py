@@ -133,6 +133,19 @@ def test_many_rows_a_slot(K, d, f, T, k, lost):
     L.close()
 
 
+@pytest.mark.parametrize("T,form", [(300, 2), (900, 4), (2600, 8)])
+@pytest.mark.parametrize("d,f,which", [(96, 2080, 0), (2080, 96, 1), (160, 2144, 0), (2144, 224, 1)])
+def test_every_width_of_tiles(d, f, which, T, form):
+    """Either product on tiles of 2, 4 and 8 feature blocks, with odd numbers of blocks, steps and half steps, and ragged slots."""
+    K = 3
+    L, w1, w2, held = make(K, K, d, f, T)
+    name = b.smoe_describe_ffn(L.handle, T).split(" | ")[which]
+    assert name.startswith(f"tile_mx_kernel<{'false' if which else 'true'}, {form},"), name
+    x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).to(DEV)
+    check(L, x, slots_of(T, K, T, skew=0.7, lost=0.05), 1, w1, w2, held)
+    L.close()
+
+
 @pytest.mark.parametrize("T", [9, 600])
 def test_scales_that_spread(T):
     """Columns of the matrices and of the rows of sizes from 2^-12 to 2^12, zero rows, zero columns."""
