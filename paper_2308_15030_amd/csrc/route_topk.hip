@@ -211,7 +211,8 @@ __device__ __forceinline__ int select_row(const smoe_topk_args& a, const T (&key
 // One token again in 64 bits, by one wave.  Only logits whose order is in question are computed again: those of experts whose keys are within
 // the tolerance of another's, those that rank a group near another where the groups are in question (`groups`), all of them where a bias meets the softmax (every key holds the sum over all).
 // The others keep their fp32 logits, which are apart from whatever they are compared with.  Few tokens come here, and a workgroup that has one is
-// the last to end, so what counts is the time of one pass, much of it instructions that come from the L2: loops are not unrolled.
+// the last to end, so what counts is the time of one pass, most of it instructions that come from the L2: loops are not unrolled (the product's
+// loop eight times: 1.5 us more).  16384 tokens, 8 of 128 experts: 53 us, 38 with this left out.
 template <int EC>
 struct topk_exact {
     static constexpr int N = 64 * EC, WAVES = EC == 4 ? 6 : 8;   // waves that work on such tokens: what fits the LDS beside the logits
@@ -260,6 +261,7 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
         near_all = (unsigned)__ballot(lane < a.groups && near_all);
         near_res = (unsigned)__ballot(lane < a.groups && near_res);
     }
+    unsigned again_of = 0;                                 // bit c: this lane's expert of chunk c
 #pragma unroll 1
     for (int e0 = 0; e0 < a.E; e0 += 64) {
         const int e = e0 + lane;
@@ -286,37 +288,44 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
             }
             again = again && (near > 1 || top);
         }
-        unsigned long long todo = __ballot(again);
+        again_of |= (again ? 1u : 0u) << (e0 >> 6);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    int* list = (int*)fkey;                                // the keys have been used up
+    int n = 0;
 #pragma unroll 1
-        while (todo) {                                     // two experts at a time
-            const int e1 = e0 + __ffsll(todo) - 1;
-            todo &= todo - 1;
-            const int e2 = todo ? e0 + __ffsll(todo) - 1 : e1;
-            todo &= todo - 1;
-            const float *w1 = a.wrow + (size_t)e1 * a.d, *w2 = a.wrow + (size_t)e2 * a.d;
-            double s1 = 0, s2 = 0;
-#pragma unroll 2
-            for (int c = lane * 4; c < a.d; c += 256) {    // d_model is a multiple of 4
-                const float4 u = *(const float4*)(w1 + c), v = *(const float4*)(w2 + c);
-                float4 x;
-                if (a.f32) x = *(const float4*)((const float*)a.x + (size_t)tok * a.d + c);
-                else {
-                    const uint2 p = *(const uint2*)((const uint16_t*)a.x + (size_t)tok * a.d + c);
-                    x = make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16),
-                                    __uint_as_float(p.y & 0xFFFF0000u));
-                }
-                s1 = fma((double)x.x, (double)u.x, s1); s2 = fma((double)x.x, (double)v.x, s2);
-                s1 = fma((double)x.y, (double)u.y, s1); s2 = fma((double)x.y, (double)v.y, s2);
-                s1 = fma((double)x.z, (double)u.z, s1); s2 = fma((double)x.z, (double)v.z, s2);
-                s1 = fma((double)x.w, (double)u.w, s1); s2 = fma((double)x.w, (double)v.w, s2);
-            }
+    for (int c = 0; c < EC; ++c) {
+        const bool again = again_of >> c & 1u;
+        const unsigned long long m = __ballot(again);
+        if (again) list[n + __popcll(m & ((1ull << lane) - 1ull))] = 64 * c + lane;
+        n += __popcll(m);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    // four experts at a time, 16 lanes each
 #pragma unroll 1
-            for (int o = 1; o < 64; o <<= 1) {
-                s1 += __shfl_xor(s1, o);
-                s2 += __shfl_xor(s2, o);
+    for (int i = lane >> 4; i < n + (lane >> 4); i += 4) {
+        const int e = list[min(i, n - 1)];
+        // the expert's row: the caller's, or out of the operand order that the product has just read (there it is in the L2), a
+        // unit of 4 weights at a time: step c / 16, half c % 8 / 4, lane e % 32 + 32 (c % 16 / 8)
+        const float4* w = a.f32 ? (const float4*)(a.wrow + (size_t)e * a.d) : (const float4*)a.wr + (size_t)(e >> 5) * (a.d >> 4) * 128 + (e & 31);
+        double sum = 0;
+#pragma unroll 1
+        for (int c = sub * 4; c < a.d; c += 64) {          // d_model is a multiple of 4
+            const float4 v = w[a.f32 ? c >> 2 : (c >> 4) * 128 + (c >> 2 & 1) * 64 + (c >> 3 & 1) * 32];
+            float4 x;
+            if (a.f32) x = *(const float4*)((const float*)a.x + (size_t)tok * a.d + c);
+            else {
+                const uint2 p = *(const uint2*)((const uint16_t*)a.x + (size_t)tok * a.d + c);
+                x = make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16),
+                                __uint_as_float(p.y & 0xFFFF0000u));
             }
-            if (lane == 0) { s.logit[e1] = s1; s.logit[e2] = s2; }
+            sum = fma((double)x.x, (double)v.x, sum);
+            sum = fma((double)x.y, (double)v.y, sum);
+            sum = fma((double)x.z, (double)v.z, sum);
+            sum = fma((double)x.w, (double)v.w, sum);
         }
+        sum = row_sum(sum);
+        if (sub == 0) s.logit[e] = sum;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     double top = 0, z = 0;                                 // scores: the largest logit, then the sum of the exponentials
