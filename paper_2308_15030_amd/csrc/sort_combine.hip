@@ -150,7 +150,6 @@ __global__ __launch_bounds__(SB) void sort_hist_kernel(const int32_t* __restrict
 
 // Position of token t = offsets[slot] + (tokens of that slot in earlier blocks)
 //                     + (in earlier waves of this block) + (in lower lanes of this wave).
-template <bool PAIRS>
 __global__ __launch_bounds__(SB) void sort_rank_kernel(const int32_t* __restrict__ slot, int T, int K,
                                                        int nblk, const int32_t* __restrict__ hist,
                                                        int32_t* __restrict__ perm,
@@ -212,8 +211,6 @@ __global__ __launch_bounds__(SB) void sort_rank_kernel(const int32_t* __restrict
         int pos = s_base[my] + s_wave[wave * K + my] + rank_in_wave;
         perm[pos] = t;
         inv_perm[t] = pos;
-    } else if (PAIRS && t < T) {
-        inv_perm[t] = -1;
     }
 }
 
@@ -464,7 +461,7 @@ int launch_permute(const smoe_config& c, const void* x, const int32_t* slot, int
         hipLaunchKernelGGL((parts == 16 ? permute_rows_kernel<16, false> : permute_rows_kernel<4, false>), dim3(parts * blocks), dim3(256), 0, s,
                            (const uint4*)x, slot, T, K, cpr, (uint4*)x_perm, perm, inv_perm, offsets, hist, nblk, 1);
     } else {
-        hipLaunchKernelGGL(sort_rank_kernel<false>, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, T, K, nblk, hist, perm,
+        hipLaunchKernelGGL(sort_rank_kernel, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, T, K, nblk, hist, perm,
                            inv_perm, offsets);
         const size_t total = (size_t)T * cpr;
         hipLaunchKernelGGL(gather_rows_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, (const uint4*)x, perm, T, cpr,
@@ -474,6 +471,79 @@ int launch_permute(const smoe_config& c, const void* x, const int32_t* slot, int
 }
 
 // ---- k choices a token (smoe_permute_topk)
+// sort_rank_kernel for pairs, of which there are many: the blocks' histograms are added up by all threads, SB / K rows of K counts at a time (65536
+// pairs, 32 slots: 21 -> 6 us), and a pair without a slot gets position -1.
+__global__ __launch_bounds__(SB) void pair_rank_kernel(const int32_t* __restrict__ slot, int n, int K, int nblk, const int32_t* __restrict__ hist,
+                                                       int32_t* __restrict__ perm, int32_t* __restrict__ inv_perm, int32_t* __restrict__ offsets) {
+    extern __shared__ int32_t sm[];
+    int32_t* s_base = sm;                    // [K]  pairs of the slot in earlier blocks, then this block's first position
+    int32_t* s_total = sm + K;               // [K]  pairs of the slot
+    int32_t* s_wave = sm + 2 * K;            // [SB_WAVES][K] per-wave counts -> exclusive prefix
+    const int tid = threadIdx.x, blk = blockIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int t = blk * SB + tid;
+    int my = t < n ? slot[t] : -1;
+    for (int i = tid; i < (2 + SB_WAVES) * K; i += SB) sm[i] = 0;
+    __syncthreads();
+    const int rows = SB / K, k0 = tid % K, r0 = tid / K;
+    if (r0 < rows) {
+        int total = 0, before = 0;
+        constexpr int U = 4;                               // rows fetched together
+        for (int b = r0; b < nblk; b += U * rows) {
+            int h[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) h[i] = hist[(size_t)min(b + i * rows, nblk - 1) * K + k0];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {                  // past the end: read again, not added
+                const int at = b + i * rows;
+                total += at < nblk ? h[i] : 0;
+                before += at < blk ? h[i] : 0;
+            }
+        }
+        if (total) atomicAdd(&s_total[k0], total);         // integers: order cannot matter
+        if (before) atomicAdd(&s_base[k0], before);
+    }
+    const bool live = (unsigned)my < (unsigned)K;          // anything else is a pair that nobody serves
+    if (!live) my = 0;
+    unsigned long long peers = __ballot(live);             // lanes of this wave that hold the same slot
+    for (int bit = 0; (1 << bit) < K; ++bit) {
+        const unsigned long long b = __ballot(live && ((my >> bit) & 1));
+        peers &= ((my >> bit) & 1) ? b : ~b;
+    }
+    const int rank_in_wave = __popcll(peers & ((1ull << lane) - 1ull));
+    if (live && rank_in_wave == 0) s_wave[wave * K + my] = __popcll(peers);
+    __syncthreads();
+    for (int k = tid; k < K; k += SB) {                    // exclusive prefix over the waves, per slot
+        int run = 0;
+#pragma unroll
+        for (int w = 0; w < SB_WAVES; ++w) {
+            const int c = s_wave[w * K + k];
+            s_wave[w * K + k] = run;
+            run += c;
+        }
+    }
+    if (wave == SB_WAVES - 1) {                            // exclusive scan over the slots, 64 at a time
+        int run = 0;
+        for (int base = 0; base < K; base += 64) {
+            const int k = base + lane, tot = k < K ? s_total[k] : 0;
+            const int incl = run + smoe_wave_incl_scan(tot);
+            if (k < K) {
+                if (blk == 0) offsets[k] = incl - tot;
+                s_base[k] += incl - tot;
+            }
+            run = __builtin_amdgcn_readlane(incl, 63);
+        }
+        if (blk == 0 && lane == 0) offsets[K] = run;
+    }
+    __syncthreads();
+    if (live) {
+        const int pos = s_base[my] + s_wave[wave * K + my] + rank_in_wave;
+        perm[pos] = t;
+        inv_perm[t] = pos;
+    } else if (t < n) {
+        inv_perm[t] = -1;
+    }
+}
+
 // x_perm[inv_perm[t * k + j], :] = x[t, :] for every choice j that is served: a row is read once and written to its places.
 __global__ __launch_bounds__(256) void scatter_rows_kernel(const uint4* __restrict__ x, const int32_t* __restrict__ inv_perm, int T, int k,
                                                            int chunks_per_row, uint4* __restrict__ x_perm) {
@@ -498,7 +568,7 @@ int launch_permute_pairs(const smoe_config& c, const void* x, const int32_t* slo
         hipLaunchKernelGGL((parts == 16 ? permute_rows_kernel<16, true> : permute_rows_kernel<4, true>), dim3(parts * blocks), dim3(256), 0, s,
                            (const uint4*)x, slot, n, K, cpr, (uint4*)x_perm, perm, inv_perm, offsets, hist, nblk, k);
     } else {
-        hipLaunchKernelGGL(sort_rank_kernel<true>, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, n, K, nblk, hist, perm,
+        hipLaunchKernelGGL(pair_rank_kernel, dim3(nblk), dim3(SB), (2 + SB_WAVES) * K * sizeof(int32_t), s, slot, n, K, nblk, hist, perm,
                            inv_perm, offsets);
         if (x_perm)
             hipLaunchKernelGGL(scatter_rows_kernel, dim3((unsigned)(((size_t)T * cpr + 255) / 256)), dim3(256), 0, s, (const uint4*)x, inv_perm,
