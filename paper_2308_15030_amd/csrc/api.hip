@@ -78,7 +78,8 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
         off = align_up(off + SMOE_FEW_T * (logits + 8 * 2) * 4, 256);
     }
     w.norm = off;    off = align_up(off + (size_t)c.E * 64 * 4, 256);      // smoe_expert_norm partial sums
-    w.rnorm = off;   off += 256;                                           // smoe_route_topk: largest norm of a router row
+    w.rnorm = off;   off += 256;                                           // smoe_route_topk: largest norm of a router row,
+    w.topk = off;    off = align_up(off + (size_t)std::min(c.max_tokens, SMOE_TOPK_FEW) * c.E * 8, 256);   // ... logits of few tokens
     // asynchronous loads from a host bank land here (copy engine) before they are packed into a slot
     w.stage = off;   off = align_up(off + (size_t)c.spare_slots * 2 * c.d_model * c.d_ff * smoe_elem_size(c.dtype), 256);
     w.total = off;
@@ -237,6 +238,7 @@ int smoe_bind(smoe_layer_t* L, const float* router_w, void* slot_w1, void* slot_
     L->router_split_done = false;
     L->d_router_norm = (float*)(L->workspace + w.rnorm);
     L->router_norm_done = false;
+    L->d_topk_logits = (double*)(L->workspace + w.topk);
     L->ws_ready = false;
     L->d_norm_partial = (float*)(L->workspace + w.norm);
     std::fill(L->slot_to_expert.begin(), L->slot_to_expert.end(), -1);

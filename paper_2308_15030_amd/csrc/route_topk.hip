@@ -20,6 +20,7 @@
 struct smoe_topk_args : smoe_route_args {
     const float* bias;
     const float* wnorm;           // largest |w_e|
+    double* logits;               // few tokens: [T, E]
     int k, sigmoid, groups, kept, best, renorm, by_logit, f32;
     int aligned;                  // a group is 4, 8, 16, 32 or 64 experts
     float scale;
@@ -219,6 +220,47 @@ struct topk_exact {
     double logit[N], score[N];                             // score: first the fp32 keys of all experts and of the resident ones
 };
 
+// Both selections of token tok by one wave from its logits in s.logit.
+template <int EC>
+__device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, topk_exact<EC>& s) {
+    const int lane = threadIdx.x & 63, sub = lane & 15, per = a.E / a.groups;
+    double top = 0, z = 0;                                 // scores: the largest logit, then the sum of the exponentials
+    if (!a.sigmoid) {
+        top = -INFINITY;
+#pragma unroll 1
+        for (int e = lane; e < a.E; e += 64) top = fmax(top, s.logit[e]);
+#pragma unroll 1
+        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+    }
+#pragma unroll 1
+    for (int e = lane; e < 64 * EC; e += 64) {
+        const double p = e >= a.E ? 0.0 : exp(a.sigmoid ? -s.logit[e] : s.logit[e] - top);
+        s.score[e] = a.sigmoid ? 1.0 / (1.0 + p) : p;
+        z += p;
+    }
+    if (!a.sigmoid) {
+#pragma unroll 1
+        for (int o = 1; o < 64; o <<= 1) z += __shfl_xor(z, o);
+    }
+    const double inv_z = a.sigmoid ? 1.0 : 1.0 / z;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    double key[EC][4];
+    int sl[EC][4], gid[EC][4];
+#pragma unroll
+    for (int c = 0; c < EC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 64 * c + 4 * sub + j, ei = min(e, a.E - 1);
+            key[c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
+            key[c][j] = e < a.E ? key[c][j] : -INFINITY;
+            sl[c][j] = e < a.E ? a.e2s[ei] : -1;
+            gid[c][j] = e / per;
+        }
+    // the first 16 lanes select among all experts, the next 16 among the resident ones
+    select_row<double, EC>(a, key, [&](int e) { return s.score[e] * inv_z; }, sl, gid, sub, tok, lane & 16,
+                           lane & 16 ? a.slot : a.orig_expert, lane & 16 ? a.gate : a.orig_gate, lane < 32, 0.0);
+}
+
 template <int EC, class AT>
 __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, AT logit_at, float err, bool groups, topk_exact<EC>& s) {
     const int lane = threadIdx.x & 63, sub = lane & 15, per = a.E / a.groups;
@@ -328,41 +370,7 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
         if (sub == 0) s.logit[e] = sum;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    double top = 0, z = 0;                                 // scores: the largest logit, then the sum of the exponentials
-    if (!a.sigmoid) {
-        top = -INFINITY;
-#pragma unroll 1
-        for (int e = lane; e < a.E; e += 64) top = fmax(top, s.logit[e]);
-#pragma unroll 1
-        for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
-    }
-#pragma unroll 1
-    for (int e = lane; e < 64 * EC; e += 64) {
-        const double p = e >= a.E ? 0.0 : exp(a.sigmoid ? -s.logit[e] : s.logit[e] - top);
-        s.score[e] = a.sigmoid ? 1.0 / (1.0 + p) : p;
-        z += p;
-    }
-    if (!a.sigmoid) {
-#pragma unroll 1
-        for (int o = 1; o < 64; o <<= 1) z += __shfl_xor(z, o);
-    }
-    const double inv_z = a.sigmoid ? 1.0 : 1.0 / z;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    double key[EC][4];
-    int sl[EC][4], gid[EC][4];
-#pragma unroll
-    for (int c = 0; c < EC; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = 64 * c + 4 * sub + j, ei = min(e, a.E - 1);
-            key[c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
-            key[c][j] = e < a.E ? key[c][j] : -INFINITY;
-            sl[c][j] = e < a.E ? a.e2s[ei] : -1;
-            gid[c][j] = e / per;
-        }
-    // the first 16 lanes select among all experts, the next 16 among the resident ones
-    select_row<double, EC>(a, key, [&](int e) { return s.score[e] * inv_z; }, sl, gid, sub, tok, lane & 16,
-                           lane & 16 ? a.slot : a.orig_expert, lane & 16 ? a.gate : a.orig_gate, lane < 32, 0.0);
+    select_exact<EC>(a, tok, s);
 }
 
 }  // namespace
@@ -537,6 +545,61 @@ int launch(const smoe_topk_args& a, hipStream_t s) {
     return launch_multi<NEB, 1, false>(a, s);
 }
 
+// Few tokens: a workgroup of the kernels above would read the whole router alone.  Here a wave takes the product of one expert with FEW_TOK tokens, in
+// 64 bits (so that nothing has to be repeated), and a second launch selects, a wave a token.
+constexpr int FEW_TOK = 4;
+
+__device__ __forceinline__ float4 load_x4(const smoe_topk_args& a, size_t at) {
+    if (a.f32) return *(const float4*)((const float*)a.x + at);
+    const uint2 p = *(const uint2*)((const uint16_t*)a.x + at);
+    return make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xFFFF0000u));
+}
+
+__global__ __launch_bounds__(256) void topk_logits_kernel(const smoe_topk_args a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int e = blockIdx.x * 4 + wave, t0 = blockIdx.y * FEW_TOK;
+    if (e >= a.E) return;
+    double sum[FEW_TOK] = {};
+#pragma unroll 2
+    for (int c = lane * 4; c < a.d; c += 256) {            // d_model is a multiple of 4
+        const float4 w = *(const float4*)(a.wrow + (size_t)e * a.d + c);
+        const double w0 = w.x, w1 = w.y, w2 = w.z, w3 = w.w;
+#pragma unroll
+        for (int i = 0; i < FEW_TOK; ++i) {                // past the batch: the last token again, not written
+            const float4 x = load_x4(a, (size_t)min(t0 + i, a.T - 1) * a.d + c);
+            sum[i] = fma((double)x.x, w0, sum[i]);
+            sum[i] = fma((double)x.y, w1, sum[i]);
+            sum[i] = fma((double)x.z, w2, sum[i]);
+            sum[i] = fma((double)x.w, w3, sum[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < FEW_TOK; ++i) {
+        double v = row_sum(sum[i]);
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+        if (lane == 0 && t0 + i < a.T) a.logits[(size_t)(t0 + i) * a.E + e] = v;
+    }
+}
+
+template <int EC>
+__global__ __launch_bounds__(64) void topk_select_kernel(const smoe_topk_args a) {
+    __shared__ topk_exact<EC> s;
+    const int lane = threadIdx.x, tok = blockIdx.x;
+    for (int e = lane; e < 64 * EC; e += 64) s.logit[e] = e < a.E ? a.logits[(size_t)tok * a.E + e] : -INFINITY;
+    float ss = 0.f;
+    for (int c = lane * 4; c < a.d; c += 256) {
+        const float4 x = load_x4(a, (size_t)tok * a.d + c);
+        ss = fmaf(x.x, x.x, ss); ss = fmaf(x.y, x.y, ss); ss = fmaf(x.z, x.z, ss); ss = fmaf(x.w, x.w, ss);
+    }
+    ss = smoe_row_sum(ss);
+    ss += __shfl_xor(ss, 16);
+    ss += __shfl_xor(ss, 32);
+    if (lane < a.k) a.xnorm[(size_t)tok * a.k + lane] = sqrtf(ss);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    select_exact<EC>(a, tok, s);
+}
+
 // Largest norm of the router's rows: a wave per row in turn, one workgroup (once per bind).
 __global__ __launch_bounds__(1024) void router_norm_kernel(const float* __restrict__ w, int E, int d, float* __restrict__ out) {
     __shared__ float s_max[16];
@@ -555,6 +618,12 @@ __global__ __launch_bounds__(1024) void router_norm_kernel(const float* __restri
         out[0] = sqrtf(big);
     }
 }
+
+// Whether T tokens take the launches for few tokens: where one workgroup's walk through the router takes longer than a second launch.  bf16 from
+// 256 KB of router on, fp32 always (its matrix products are slow).  Measured with 2 choices (us, one launch / two): bf16, 64 experts of 768 columns,
+// 1 token 8.1 / 8.3, 128 tokens 9.1 / 9.6; 128 of 1024 13.4 / 9.7 and 15.1 / 12.9 (256 tokens: 15.3 / 16.9); 256 of 2048 38 / 15 and 40 / 26; fp32, 64 of
+// 768 14.1 / 7.6 and 17.6 / 8.7.
+bool topk_few(const smoe_config& c, int T) { return T <= SMOE_TOPK_FEW && (c.dtype == SMOE_F32 || c.E * c.d_model > 65536); }
 
 }  // namespace
 
@@ -589,6 +658,14 @@ int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, cons
     const int n = a.f32 ? 4 * (((c.d_model + 7) / 8 + slices - 1) / slices) : 3 * ((c.d_model / 16 + slices - 1) / slices);
     a.err_norm = a.f32 ? 1.5f : 1.f;
     a.err_sum = 1.f + 0.1f * n;
+    if (topk_few(c, T)) {
+        a.logits = L->d_topk_logits;
+        hipLaunchKernelGGL(topk_logits_kernel, dim3((c.E + 3) / 4, (T + FEW_TOK - 1) / FEW_TOK), dim3(256), 0, s, a);
+        if (int rc = smoe_check_hip(hipGetLastError(), "smoe_route_topk: logits launch")) return rc;
+        const auto select = c.E <= 64 ? topk_select_kernel<1> : c.E <= 128 ? topk_select_kernel<2> : topk_select_kernel<4>;
+        hipLaunchKernelGGL(select, dim3(T), dim3(64), 0, s, a);
+        return smoe_check_hip(hipGetLastError(), "smoe_route_topk: selection launch");
+    }
     if (c.E <= 32) return launch<1>(a, s);
     if (c.E <= 64) return launch<2>(a, s);
     if (c.E <= 128) return launch<4>(a, s);

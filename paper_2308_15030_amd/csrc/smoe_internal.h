@@ -86,6 +86,7 @@ struct smoe_layer {
     bool router_split_done = false;          // made by the first smoe_route after a bind
     float* d_router_norm = nullptr;          // largest |w_e| of the router's rows (smoe_route_topk)
     bool router_norm_done = false;           // made by the first smoe_route_topk after a bind
+    double* d_topk_logits = nullptr;         // smoe_route_topk on at most SMOE_TOPK_FEW tokens: [tokens, E]
 
     hipEvent_t prof_ev[4] = {nullptr, nullptr, nullptr, nullptr};   // one-shot FFN profiling events
     hipEvent_t bracket[2] = {nullptr, nullptr};                     // smoe_profile_begin / _end
@@ -100,7 +101,7 @@ struct smoe_layer {
 };
 
 struct smoe_ws_layout {
-    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, rnorm, stage, total;
+    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, rnorm, topk, stage, total;
 };
 smoe_ws_layout smoe_ws_plan(const smoe_config& c);
 
@@ -147,6 +148,7 @@ inline size_t smoe_scale_pitch(int d) { return ((size_t)d / 32 + 7) / 8 * 8; }  
 // whose rows (8 elements of padding each) fit the dynamic LDS of a compute unit; the path keeps the hidden
 // activations of every slot for every token of the batch, in blocks of 32 tokens.
 constexpr int SMOE_SMALL_T = 128;
+constexpr int SMOE_TOPK_FEW = 128;                         // most tokens of smoe_route_topk's launches for few tokens
 constexpr int SMOE_FEW_T = 16;                             // ... and at most this many take its launches for few tokens
 constexpr int SMOE_SMALL_LDS = 160 * 1024 - 2048;          // the rest covers the static tables
 inline size_t smoe_small_batch_rows(const smoe_config& c) {
