@@ -18,10 +18,12 @@ extern "C" {
 
 /* E_memory of Appendix A.1: memory is the sum over the resident experts, plus
  * what the layer needs besides them.  All in bytes, from the shape alone:
- *   expert_bytes     one expert's two matrices, 2 * d_model * d_ff * sizeof(dtype)
+ *   expert_bytes     one expert's two matrices in a slot, 2 * d_model * d_ff * sizeof(dtype);
+ *                    about 33/64 of the bf16 figure for SMOE_MXFP8
  *   resident_bytes   (K + spare_slots) * expert_bytes, the slot arrays in GPU memory
  *   workspace_bytes  smoe_workspace_bytes() for this shape
- *   bank_bytes       E * expert_bytes, the full bank kept in external memory
+ *   bank_bytes       E * 2 * d_model * d_ff * sizeof(dtype) (SMOE_MXFP8: of bf16), the
+ *                    full bank kept in external memory
  *   router_bytes     E * d_model * 4                                           */
 typedef struct {
     uint64_t expert_bytes, resident_bytes, workspace_bytes, bank_bytes, router_bytes;
@@ -50,7 +52,8 @@ int smoe_period_inflection(const float* latency_us /*host*/, int n, float tolera
 /* Calibration for the rooflines this library is measured against (not part of
  * the paper's method): enqueues a kernel that does nothing but read the first K
  * slots of the first (which = 0) or second (which = 1) slot array once --
- * K * d_model * d_ff * sizeof(dtype) bytes, the bytes the weight-streaming
+ * K * d_model * d_ff * sizeof(dtype) bytes (SMOE_MXFP8: K slots as
+ * smoe_slot_weight_bytes counts them), the bytes the weight-streaming
  * kernels of a decode step read when every slot is active -- with plain
  * coalesced loads.  Bracket it with smoe_profile_begin / _end: the elapsed time
  * is what a launch that moves these bytes costs on this GPU with no arithmetic
@@ -58,7 +61,7 @@ int smoe_period_inflection(const float* latency_us /*host*/, int n, float tolera
 int smoe_profile_stream_read(smoe_layer_t* layer, int which, void* stream);
 
 /* Measurement aid (not part of the paper's method): HIP events for the NEXT
- * smoe_expert_ffn (or smoe_forward) call on this handle.  The call attaches
+ * smoe_expert_ffn, smoe_expert_ffn_mx or smoe_forward call on this handle.  The call attaches
  * them to its two product kernels' own dispatches: g1_begin / g1_end take the
  * start and end of the first product's execution, g2_begin / g2_end those of
  * the second, so hipEventElapsedTime(g1_begin, g1_end) is that kernel's

@@ -67,7 +67,9 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
     // hidden activations: every segment is re-based to a multiple of 32 rows
     const size_t rows = std::max((size_t)c.max_tokens + 32 * (size_t)c.K, smoe_small_batch_rows(c));
     const size_t hidden = c.dtype == SMOE_MXFP8 ? smoe_mx_hidden_bytes(c) : rows * c.d_ff * smoe_elem_size(c.dtype);
-    w.hidden = off;  off = align_up(off + hidden, 256);
+    // (in front of a pass's products, smoe_route_topk keeps the logits of few tokens there)
+    const size_t logits64 = (size_t)std::min(c.max_tokens, SMOE_TOPK_FEW) * c.E * 8;
+    w.hidden = off;  off = align_up(off + std::max(hidden, logits64), 256);
     // bf16 activations: the router's weights in matrix-operand order, experts padded to a multiple of 32
     w.rsplit = off;
     if (c.dtype != SMOE_F32) off = align_up(off + (size_t)((c.E + 31) / 32 * 32) * c.d_model * 4, 256);
@@ -78,8 +80,7 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
         off = align_up(off + SMOE_FEW_T * (logits + 8 * 2) * 4, 256);
     }
     w.norm = off;    off = align_up(off + (size_t)c.E * 64 * 4, 256);      // smoe_expert_norm partial sums
-    w.rnorm = off;   off += 256;                                           // smoe_route_topk: largest norm of a router row,
-    w.topk = off;    off = align_up(off + (size_t)std::min(c.max_tokens, SMOE_TOPK_FEW) * c.E * 8, 256);   // ... logits of few tokens
+    w.rnorm = off;   off += 256;                                           // smoe_route_topk: largest norm of a router row
     // asynchronous loads from a host bank land here (copy engine) before they are packed into a slot
     w.stage = off;   off = align_up(off + (size_t)c.spare_slots * 2 * c.d_model * c.d_ff * smoe_elem_size(c.dtype), 256);
     w.total = off;
@@ -237,8 +238,7 @@ int smoe_bind(smoe_layer_t* L, const float* router_w, void* slot_w1, void* slot_
     L->d_route_part = L->workspace + w.rpart;
     L->router_split_done = false;
     L->d_router_norm = (float*)(L->workspace + w.rnorm);
-    L->router_norm_done = false;
-    L->d_topk_logits = (double*)(L->workspace + w.topk);
+    L->router_topk_done = false;
     L->ws_ready = false;
     L->d_norm_partial = (float*)(L->workspace + w.norm);
     std::fill(L->slot_to_expert.begin(), L->slot_to_expert.end(), -1);

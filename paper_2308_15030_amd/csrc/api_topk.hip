@@ -61,16 +61,15 @@ int smoe_route_topk(smoe_layer_t* L, const smoe_topk_rule* rule, const float* bi
     if (smoe_misaligned(x, 16)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: x must be 16-byte aligned");
     if (smoe_misaligned(bias, 4)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: bias must be 4-byte aligned");
     const hipStream_t s = (hipStream_t)stream;
-    const bool split = c.dtype != SMOE_F32 && !L->router_split_done, norm = !L->router_norm_done;
-    if (split || norm) {
-        // a capture only records the preparation: the next call outside of it still has to run its own
+    if (!L->router_topk_done) {
+        // a capture only records the preparation: the next call outside of it still has to run its own, also where a smoe_route in a
+        // capture has recorded the router's weights already
         hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
         if (int rc = smoe_check_hip(hipStreamIsCapturing(s, &capture), "smoe_route_topk: capture status")) return rc;
-        if (split)
+        if (c.dtype != SMOE_F32)
             if (int rc = smoe_launch_split_router(L, s)) return rc;
-        if (norm)
-            if (int rc = smoe_launch_router_norm(L, s)) return rc;
-        if (capture == hipStreamCaptureStatusNone) L->router_split_done = L->router_norm_done = true;
+        if (int rc = smoe_launch_router_norm(L, s)) return rc;
+        if (capture == hipStreamCaptureStatusNone) L->router_split_done = L->router_topk_done = true;
     }
     return smoe_launch_route_topk(L, r, bias, x, T, orig_expert, orig_gate, slot, gate, xnorm, s);
 }
@@ -98,6 +97,7 @@ int smoe_expert_ffn_mx(smoe_layer_t* L, const void* q, const void* q_scale, cons
         return smoe_fail(SMOE_EINVAL, "smoe_expert_ffn_mx: q and y_perm must be 16-byte aligned, scales 8-byte");
     const int rc = smoe_launch_ffn_mx(L, q, q_scale, perm, k, offsets, T, y_perm, (hipStream_t)stream);
     smoe_note_slot_pass(L);
+    L->prof_ev[0] = L->prof_ev[1] = L->prof_ev[2] = L->prof_ev[3] = nullptr;
     return rc;
 }
 

@@ -565,39 +565,39 @@ __global__ __launch_bounds__(256) void pack_mx_kernel(const uint16_t* __restrict
 }
 
 template <bool FIRST, int NW, int BATCH, bool NT>
-int launch_stream_as(const MxArgs& g, hipStream_t s) {
+int launch_stream_as(const MxArgs& g, hipStream_t s, const hipEvent_t* e) {
     const size_t tiles = (size_t)(g.rows / 32 + std::min(g.nslots, g.rows));   // an upper bound of the sum of ceil(len / 32)
-    hipLaunchKernelGGL((stream_mx_kernel<FIRST, NW, BATCH, NT>), dim3((unsigned)(tiles * (g.N / 32))), dim3(64 * NW), 0, s, g);
+    smoe_launch_timed(stream_mx_kernel<FIRST, NW, BATCH, NT>, dim3((unsigned)(tiles * (g.N / 32))), dim3(64 * NW), s, e[0], e[1], g);
     return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
 }
 
 template <bool FIRST>
-int launch_stream(const MxArgs& g, hipStream_t s) {
+int launch_stream(const MxArgs& g, hipStream_t s, const hipEvent_t* e) {
     // Two waves to a feature block, of two steps a batch, for short reductions; four, of four steps, from 25 steps on, where a wave has more to ask for.
     // (us; 10 slots of 768 x 3072, 13 tokens: first product 7.4 with four steps a batch, 6.8 with two, 7.8 with four waves, and 13.8 with eight of four
     // steps; second product 7.0 with four waves of four steps, 7.2 of two, 8.0 with two waves, 7.7 with eight; 16 slots, 32 tokens: 12.5, 10.3, 12.3 and 21.8;
     // 10.5, 12.9, 10.2 and 13.2)
-    if (smoe_mx_steps(g.R) <= 24) return g.past ? launch_stream_as<FIRST, 2, 2, true>(g, s) : launch_stream_as<FIRST, 2, 2, false>(g, s);
-    return g.past ? launch_stream_as<FIRST, 4, 4, true>(g, s) : launch_stream_as<FIRST, 4, 4, false>(g, s);
+    if (smoe_mx_steps(g.R) <= 24) return g.past ? launch_stream_as<FIRST, 2, 2, true>(g, s, e) : launch_stream_as<FIRST, 2, 2, false>(g, s, e);
+    return g.past ? launch_stream_as<FIRST, 4, 4, true>(g, s, e) : launch_stream_as<FIRST, 4, 4, false>(g, s, e);
 }
 
 template <bool FIRST, int FB, int ST>
-int launch_tile(const MxArgs& g, hipStream_t s) {
+int launch_tile(const MxArgs& g, hipStream_t s, const hipEvent_t* e) {
     static smoe_lds_raised raised;
     constexpr size_t lds = TileShape<FB, ST>::LDS;
     if (int rc = raised.ensure((const void*)tile_mx_kernel<FIRST, FB, ST>, lds, (int)lds)) return rc;
-    hipLaunchKernelGGL((tile_mx_kernel<FIRST, FB, ST>), dim3(2 * g.cus), dim3(256), lds, s, g);
+    smoe_launch_timed_lds(tile_mx_kernel<FIRST, FB, ST>, dim3(2 * g.cus), dim3(256), lds, s, e[0], e[1], g);
     return smoe_check_hip(hipGetLastError(), FIRST ? "smoe_expert_ffn_mx: first product launch" : "smoe_expert_ffn_mx: second product launch");
 }
 
 template <bool FIRST>
-int launch_product(const MxArgs& g, hipStream_t s) {
+int launch_product(const MxArgs& g, hipStream_t s, const hipEvent_t* e) {
     switch (smoe_mx_form(g.rows, g.nslots, g.N)) {
-        case 8: return launch_tile<FIRST, 8, 3>(g, s);
-        case 4: return launch_tile<FIRST, 4, 3>(g, s);
-        case 2: return launch_tile<FIRST, 2, 4>(g, s);
+        case 8: return launch_tile<FIRST, 8, 3>(g, s, e);
+        case 4: return launch_tile<FIRST, 4, 3>(g, s, e);
+        case 2: return launch_tile<FIRST, 2, 4>(g, s, e);
     }
-    return launch_stream<FIRST>(g, s);
+    return launch_stream<FIRST>(g, s, e);
 }
 
 }  // namespace
@@ -640,14 +640,14 @@ int smoe_launch_ffn_mx(const smoe_layer* L, const void* q, const void* q_scale, 
     g.h = h;
     g.hs = hs;
     g.y = (uint16_t*)y_perm;
-    g.cus = 256;
+    g.cus = 256;                                               // of the whole GPU; a multiple of the 8 dies (tile_mx_kernel)
     g.past = smoe_weights_outgrow_cache(L);
-    int rc = launch_product<true>(g, s);
+    int rc = launch_product<true>(g, s, L->prof_ev);
     if (rc) return rc;
     g.x = h;
     g.xs = hs;
     g.w = (const uint8_t*)L->slot_w2;
     g.R = c.d_ff;
     g.N = c.d_model;
-    return launch_product<false>(g, s);
+    return launch_product<false>(g, s, L->prof_ev + 2);
 }

@@ -659,7 +659,7 @@ int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, cons
     a.err_norm = a.f32 ? 1.5f : 1.f;
     a.err_sum = 1.f + 0.1f * n;
     if (topk_few(c, T)) {
-        a.logits = L->d_topk_logits;
+        a.logits = (double*)L->d_hidden;                   // scratch that the products after it fill
         hipLaunchKernelGGL(topk_logits_kernel, dim3((c.E + 3) / 4, (T + FEW_TOK - 1) / FEW_TOK), dim3(256), 0, s, a);
         if (int rc = smoe_check_hip(hipGetLastError(), "smoe_route_topk: logits launch")) return rc;
         const auto select = c.E <= 64 ? topk_select_kernel<1> : c.E <= 128 ? topk_select_kernel<2> : topk_select_kernel<4>;

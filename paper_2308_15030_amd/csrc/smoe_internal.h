@@ -85,8 +85,7 @@ struct smoe_layer {
     void* d_route_part = nullptr;            // small batches: partial logits and sums of squares of at most SMOE_FEW_T tokens
     bool router_split_done = false;          // made by the first smoe_route after a bind
     float* d_router_norm = nullptr;          // largest |w_e| of the router's rows (smoe_route_topk)
-    bool router_norm_done = false;           // made by the first smoe_route_topk after a bind
-    double* d_topk_logits = nullptr;         // smoe_route_topk on at most SMOE_TOPK_FEW tokens: [tokens, E]
+    bool router_topk_done = false;           // it and d_router_split, made by the first smoe_route_topk after a bind
 
     hipEvent_t prof_ev[4] = {nullptr, nullptr, nullptr, nullptr};   // one-shot FFN profiling events
     hipEvent_t bracket[2] = {nullptr, nullptr};                     // smoe_profile_begin / _end
@@ -101,7 +100,7 @@ struct smoe_layer {
 };
 
 struct smoe_ws_layout {
-    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, rnorm, topk, stage, total;
+    size_t e2s, s2e, phys, dplan, hist, hist32, hidden, rsplit, rpart, norm, rnorm, stage, total;
 };
 smoe_ws_layout smoe_ws_plan(const smoe_config& c);
 
