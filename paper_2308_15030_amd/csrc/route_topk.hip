@@ -23,25 +23,29 @@ struct smoe_topk_args : smoe_route_args {
     double* logits;               // few tokens: [T, E]
     int k, sigmoid, groups, kept, best, renorm, by_logit, f32;
     int aligned;                  // a group is 4, 8, 16, 32 or 64 experts
-    float scale;
+    float scale, inv_per;         // 1 / experts of a group
     float err_norm, err_sum;      // estimated error of a logit in units of 2^-24: of |x| |w|, and of the sum of its slices' magnitudes
 };
 
 namespace {
 
 __device__ __forceinline__ float sigmoid_of(float v) { return 1.0f / (1.0f + expf(-v)); }
+// The same in a few instructions, for keys: the exponent is off by 1.5 2^-24 of its size (the constant and the product), the two instructions by a unit
+// of 2^-23 each, the sum by half of one.
+__device__ __forceinline__ float sigmoid_near(float v) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
+}
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+__device__ __forceinline__ int larger(int a, int b) { return max(a, b); }
+__device__ __forceinline__ int smaller(int a, int b) { return min(a, b); }
 __device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
 __device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
 
-// The rotations and reductions of wave_ops.h in 64 bits.
-template <int N>
-__device__ __forceinline__ float row_ror(float v) { return smoe_row_ror<N>(v); }
-template <int N>
-__device__ __forceinline__ double row_ror(double v) {
-    return __hiloint2double(smoe_row_ror<N>(__double2hiint(v)), smoe_row_ror<N>(__double2loint(v)));
-}
+// A lane's value from another of its row, by the control word of the instruction (0x120 + n: the row turned by n lanes), and the reductions of
+// wave_ops.h in 64 bits.
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_mov_dpp(v, CTRL, 0xf, 0xf, true); }
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true)); }
 template <int CTRL>
@@ -49,39 +53,92 @@ __device__ __forceinline__ double dpp(double v) {
     return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xf, 0xf, true),
                             __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xf, 0xf, true));
 }
+// ... of integers each step is one instruction (a maximum of floats first quietens its operands, and takes three).
 template <class T>
 __device__ __forceinline__ T row_max(T v) {
-    v = larger(v, row_ror<8>(v));
-    v = larger(v, row_ror<4>(v));
-    v = larger(v, row_ror<2>(v));
-    return larger(v, row_ror<1>(v));
+    v = larger(v, dpp<0x128>(v));
+    v = larger(v, dpp<0x124>(v));
+    v = larger(v, dpp<0x122>(v));
+    return larger(v, dpp<0x121>(v));
 }
 template <class T>
+__device__ __forceinline__ T row_min(T v) {
+    v = smaller(v, dpp<0x128>(v));
+    v = smaller(v, dpp<0x124>(v));
+    v = smaller(v, dpp<0x122>(v));
+    return smaller(v, dpp<0x121>(v));
+}
+template <class T, int R>
+__device__ __forceinline__ void row_max(T (&v)[R]) {       // step by step of all of them
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], dpp<0x128>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], dpp<0x124>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], dpp<0x122>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], dpp<0x121>(v[r]));
+}
+template <int R>
+__device__ __forceinline__ void row_min(int (&v)[R]) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = min(v[r], dpp<0x128>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = min(v[r], dpp<0x124>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = min(v[r], dpp<0x122>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = min(v[r], dpp<0x121>(v[r]));
+}
+// Integers in the order of the floats, and back; a float that is no number becomes -infinity.
+__device__ __forceinline__ int ordered_bits(int i) { return i ^ (i >> 31 & 0x7fffffff); }
+__device__ __forceinline__ int to_ordered(float v) { return ordered_bits(__float_as_int(fmaxf(v, -INFINITY))); }
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(ordered_bits(i)); }
+// What keys are compared as: floats as integers in their order, doubles as they are.
+template <class T>
+struct key_order {
+    using type = T;
+    static __device__ __forceinline__ T of(T v) { return v; }
+    static __device__ __forceinline__ T value(T v) { return v; }
+};
+template <>
+struct key_order<float> {
+    using type = int;
+    static __device__ __forceinline__ int of(float v) { return to_ordered(v); }
+    static __device__ __forceinline__ float value(int v) { return from_ordered(v); }
+};
+
+template <class T>
 __device__ __forceinline__ T row_sum(T v) {
-    v += row_ror<8>(v);
-    v += row_ror<4>(v);
-    v += row_ror<2>(v);
-    return v + row_ror<1>(v);
+    v += dpp<0x128>(v);
+    v += dpp<0x124>(v);
+    v += dpp<0x122>(v);
+    return v + dpp<0x121>(v);
 }
 
-// The best experts by key of one token, in its 16 lanes: lane `sub` is left with choice number `sub` in `mine` (-1: none).  Returns what was
-// decided by a distance of at most tol (twice that between sums of two): 1 the choices, 2 the groups.  gid: group of each of the lane's experts.
+// e / (E / groups): e + 1/2 is at least 1/(2 per) from the next border, far more than the product's rounding
+__device__ __forceinline__ int group_of(const smoe_topk_args& a, int e) { return (int)(((float)e + 0.5f) * a.inv_per); }
+
+// The groups a token keeps, in its 16 lanes: the keys of all other experts become none.  Returns 2 where that was decided by a distance of at most
+// tol (twice that between sums of two).
 template <class T, int EC>
-__device__ __forceinline__ int pick_row(T (&key)[EC][4], const int (&gid)[EC][4], const smoe_topk_args& a, int sub, T tol, int& mine) {
-    const T none = -INFINITY;
+__device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC][4], const smoe_topk_args& a, int sub, T tol) {
+    using O = key_order<T>;
+    using I = typename O::type;
+    const I none = O::of(-INFINITY);
     int close = 0;
     if (a.groups > 1 && a.aligned) {
         // Groups of 4, 8, .. 64 experts: 1, 2, .. 16 neighbouring lanes of one of the lane's packs of four, so each lane finds the rank of its
         // own groups with the steps of one reduction, and counts the groups in front of each (16384 tokens, 8 groups of 16: 18 us
         // less than the walk over the groups below).
-        T rank[EC];
+        I rank[EC];
         const int lanes = a.E / a.groups >> 2;
 #pragma unroll
         for (int c = 0; c < EC; ++c) {
-            const T hi0 = larger(key[c][0], key[c][1]), lo0 = smaller(key[c][0], key[c][1]);
-            const T hi1 = larger(key[c][2], key[c][3]), lo1 = smaller(key[c][2], key[c][3]);
-            T m1 = larger(hi0, hi1), m2 = larger(smaller(hi0, hi1), larger(lo0, lo1));
-            auto merge = [&](T o1, T o2) {
+            const I hi0 = larger(key[c][0], key[c][1]), lo0 = smaller(key[c][0], key[c][1]);
+            const I hi1 = larger(key[c][2], key[c][3]), lo1 = smaller(key[c][2], key[c][3]);
+            I m1 = larger(hi0, hi1), m2 = larger(smaller(hi0, hi1), larger(lo0, lo1));
+            auto merge = [&](I o1, I o2) {
                 m2 = larger(smaller(m1, o1), larger(m2, o2));
                 m1 = larger(m1, o1);
             };
@@ -89,7 +146,7 @@ __device__ __forceinline__ int pick_row(T (&key)[EC][4], const int (&gid)[EC][4]
             if (lanes >= 4) merge(dpp<0x4E>(m1), dpp<0x4E>(m2));
             if (lanes >= 8) merge(dpp<0x141>(m1), dpp<0x141>(m2));   // the other quad of eight lanes
             if (lanes >= 16) merge(dpp<0x140>(m1), dpp<0x140>(m2));  // the other eight
-            rank[c] = a.best == 2 && m2 > none ? m1 + m2 : m1;
+            rank[c] = a.best == 2 && m2 > none ? O::of(O::value(m1) + O::value(m2)) : m1;
         }
         int ahead[EC];
 #pragma unroll
@@ -98,7 +155,7 @@ __device__ __forceinline__ int pick_row(T (&key)[EC][4], const int (&gid)[EC][4]
             const int at = ((threadIdx.x - s) & 15) | (threadIdx.x & 48);
 #pragma unroll
             for (int o = 0; o < EC; ++o) {
-                const T v = __shfl(rank[o], at);
+                const I v = __shfl(rank[o], at);
 #pragma unroll
                 for (int c = 0; c < EC; ++c) {
                     const bool before = o < c || (o == c && ((at ^ threadIdx.x) & 15) && (at & 15) < (int)(threadIdx.x & 15));
@@ -106,94 +163,128 @@ __device__ __forceinline__ int pick_row(T (&key)[EC][4], const int (&gid)[EC][4]
                 }
             }
         }
-        T worst = INFINITY, next = none;
+        I worst = O::of(T(INFINITY)), next = none;
 #pragma unroll
         for (int c = 0; c < EC; ++c) {
             if (64 * c >= a.E) continue;                   // uniform
             const bool in = 64 * c + 4 * sub < a.E;
             const bool keep = in && ahead[c] < a.kept && rank[c] > none;
-            worst = smaller(worst, in && ahead[c] < a.kept ? rank[c] : T(INFINITY));
+            worst = smaller(worst, in && ahead[c] < a.kept ? rank[c] : O::of(T(INFINITY)));
             next = larger(next, in && ahead[c] >= a.kept ? rank[c] : none);
 #pragma unroll
             for (int j = 0; j < 4; ++j) key[c][j] = keep ? key[c][j] : none;
         }
-        close = -row_max(-worst) - row_max(next) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;   // (two empty groups: NaN, not close)
+        close = O::value(row_min(worst)) - O::value(row_max(next)) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;   // (two empty groups: NaN, not close)
     } else if (a.groups > 1) {
-        T rank = none;                                     // of group `sub`
+        I rank = none;                                     // of group `sub`
+        int gid[EC][4];
+#pragma unroll
+        for (int c = 0; c < EC; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) gid[c][j] = group_of(a, 64 * c + 4 * sub + j);
         for (int g = 0; g < a.groups; ++g) {
-            T m1 = none, m2 = none;                        // the two largest keys of the group
+            I m1 = none, m2 = none;                        // the two largest keys of the group
 #pragma unroll
             for (int c = 0; c < EC; ++c)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const T v = gid[c][j] == g ? key[c][j] : none;
+                    const I v = gid[c][j] == g ? key[c][j] : none;
                     m2 = larger(m2, smaller(m1, v));
                     m1 = larger(m1, v);
                 }
-            auto merge = [&](T o1, T o2) {
+            auto merge = [&](I o1, I o2) {
                 m2 = larger(smaller(m1, o1), larger(m2, o2));
                 m1 = larger(m1, o1);
             };
-            merge(row_ror<8>(m1), row_ror<8>(m2));
-            merge(row_ror<4>(m1), row_ror<4>(m2));
-            merge(row_ror<2>(m1), row_ror<2>(m2));
-            merge(row_ror<1>(m1), row_ror<1>(m2));
-            const T r = a.best == 2 && m2 > none ? m1 + m2 : m1;
+            merge(dpp<0x128>(m1), dpp<0x128>(m2));
+            merge(dpp<0x124>(m1), dpp<0x124>(m2));
+            merge(dpp<0x122>(m1), dpp<0x122>(m2));
+            merge(dpp<0x121>(m1), dpp<0x121>(m2));
+            const I r = a.best == 2 && m2 > none ? O::of(O::value(m1) + O::value(m2)) : m1;
             rank = g == sub ? r : rank;
         }
         unsigned kept = 0;
-        T last = INFINITY;
+        I last = O::of(T(INFINITY));
         for (int i = 0; i < a.kept; ++i) {
             last = row_max(rank);
-            const int w = smoe_row_min(rank == last ? sub : 99);
+            const int w = row_min(rank == last ? sub : 99);
             if (last > none) kept |= 1u << (w & 31);
             rank = w == sub ? none : rank;
         }
-        close = last - row_max(rank) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;
+        close = O::value(last) - O::value(row_max(rank)) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
 #pragma unroll
             for (int j = 0; j < 4; ++j) key[c][j] = (kept >> (gid[c][j] & 31)) & 1u ? key[c][j] : none;
     }
-    mine = -1;
-    T last = INFINITY;
+    return close;
+}
+
+// The best experts by key of one token, in its 16 lanes, of R lists of keys at once (one's steps fill the other's waits): lane `sub` is left with
+// choice number `sub` of each in `mine` (-1: none).  Returns whether a choice was decided by a distance of at most tol.
+template <class T, int EC, int R>
+__device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC][4], const smoe_topk_args& a, int sub, T tol, int (&mine)[R]) {
+    using O = key_order<T>;
+    using I = typename O::type;
+    const I none = O::of(-INFINITY);
+    int close = 0;
+    T last[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        mine[r] = -1;
+        last[r] = INFINITY;
+    }
+#pragma unroll 1
     for (int i = 0; i <= a.k; ++i) {                       // one round more than choices: the distance to the next best
-        T m = none;
+        I m[R];
 #pragma unroll
-        for (int c = 0; c < EC; ++c)
+        for (int r = 0; r < R; ++r) {
+            m[r] = none;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m = larger(m, key[c][j]);
-        m = row_max(m);
-        close |= last - m <= tol ? 1 : 0;
-        last = m;
-        if (i == a.k) break;                               // uniform
-        int e = INT_MAX;
+            for (int c = 0; c < EC; ++c)
 #pragma unroll
-        for (int c = EC - 1; c >= 0; --c)
+                for (int j = 0; j < 4; ++j) m[r] = larger(m[r], key[r][c][j]);
+        }
+        row_max(m);
 #pragma unroll
-            for (int j = 3; j >= 0; --j) e = key[c][j] == m ? 64 * c + 4 * sub + j : e;
-        e = smoe_row_min(e);
-        mine = m > none && i == sub ? e : mine;
+        for (int r = 0; r < R; ++r) {
+            const T v = O::value(m[r]);
+            close |= last[r] - v <= tol ? 1 : 0;
+            last[r] = v;
+        }
+        int at[R], e[R];                                   // the lane's first expert with that key; the row's first loses it
 #pragma unroll
-        for (int c = 0; c < EC; ++c)
+        for (int r = 0; r < R; ++r) {
+            at[r] = INT_MAX;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) key[c][j] = 64 * c + 4 * sub + j == e ? none : key[c][j];
+            for (int c = EC - 1; c >= 0; --c)
+#pragma unroll
+                for (int j = 3; j >= 0; --j) at[r] = key[r][c][j] == m[r] ? 64 * c + j : at[r];
+            e[r] = at[r] == INT_MAX ? at[r] : at[r] + 4 * sub;
+        }
+        int own[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) own[r] = e[r];
+        row_min(e);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mine[r] = m[r] > none && i == sub && i < a.k ? e[r] : mine[r];
+            int gone = own[r] == e[r] ? at[r] : -1;
+            asm("" : "+v"(gone));                          // one comparison a key below, not two and their conjunction
+#pragma unroll
+            for (int c = 0; c < EC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) key[r][c][j] = gone == 64 * c + j ? none : key[r][c][j];
+        }
     }
     return close;
 }
 
-// A selection of token tok in its 16 lanes: among the resident experts with `served`, else among all.  score_at: an expert's score.  Returns
-// what pick_row does; store: write the results to id and gate.
-template <class T, int EC, class AT>
-__device__ __forceinline__ int select_row(const smoe_topk_args& a, const T (&key)[EC][4], AT score_at, const int (&sl)[EC][4],
-                                          const int (&gid)[EC][4], int sub, int tok, bool served, int32_t* id, float* gate, bool store, T tol) {
-    T kk[EC][4];
-#pragma unroll
-    for (int c = 0; c < EC; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) kk[c][j] = served && sl[c][j] < 0 ? T(-INFINITY) : key[c][j];
-    int mine;
-    const int close = pick_row<T, EC>(kk, gid, a, sub, tol, mine);
+// What lane `sub` has chosen: weight and identity, among the resident experts with `served`, else among all.  score_at: an expert's score.  store: write
+// the results to id and gate.
+template <class T, class AT>
+__device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, AT score_at, int sub, int tok, bool served, int32_t* id, float* gate,
+                                             bool store) {
     const int e = min(max(mine, 0), a.E - 1);
     T w = 0;
     if (mine >= 0) w = score_at(e);
@@ -206,16 +297,16 @@ __device__ __forceinline__ int select_row(const smoe_topk_args& a, const T (&key
         id[at] = !served ? e : mine < 0 ? -1 : a.e2s[e];   // (a token whose logits are all NaN: expert 0, weight 0)
         gate[at] = (float)(w * a.scale);
     }
-    return close;
 }
 
 // One token again in 64 bits, by one wave.  Only logits whose order is in question are computed again: those of experts whose keys are within
 // the tolerance of another's, those that rank a group near another where the groups are in question (`groups`), all of them where a bias meets the softmax (every key holds the sum over all).
 // The others keep their fp32 logits, which are apart from whatever they are compared with.  Few tokens come here, and a workgroup that has one is
-// the last to end, so what counts is the time of one pass, most of it instructions that come from the L2: loops are not unrolled (the product's
-// loop eight times: 1.5 us more).  16384 tokens, 8 of 128 experts: 53 us, 38 with this left out.
+// the last to end, so what counts is the time of one pass: 27000 cycles with two logits to repeat (16384 tokens, 8 of 128 experts: 11 of 53 us), of
+// which 1500 for the keys, 500 for the groups, 5300 for the distances, 3900 for the products and 14000 for the selection, whose code comes from memory
+// for the first time.  Loads go together, 4 or 8 at a time (one at a time: 36000 cycles), but loops are not unrolled further.
 template <int EC>
-struct topk_exact {
+struct alignas(16) topk_exact {
     static constexpr int N = 64 * EC, WAVES = EC == 4 ? 6 : 8;   // waves that work on such tokens: what fits the LDS beside the logits
     double logit[N], score[N];                             // score: first the fp32 keys of all experts and of the resident ones
 };
@@ -223,7 +314,7 @@ struct topk_exact {
 // Both selections of token tok by one wave from its logits in s.logit.
 template <int EC>
 __device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, topk_exact<EC>& s) {
-    const int lane = threadIdx.x & 63, sub = lane & 15, per = a.E / a.groups;
+    const int lane = threadIdx.x & 63, sub = lane & 15;
     double top = 0, z = 0;                                 // scores: the largest logit, then the sum of the exponentials
     if (!a.sigmoid) {
         top = -INFINITY;
@@ -244,26 +335,41 @@ __device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, t
     }
     const double inv_z = a.sigmoid ? 1.0 : 1.0 / z;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    double key[EC][4];
-    int sl[EC][4], gid[EC][4];
+    double key[1][EC][4];
+    int sl[EC][4];
 #pragma unroll
     for (int c = 0; c < EC; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int e = 64 * c + 4 * sub + j, ei = min(e, a.E - 1);
-            key[c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
-            key[c][j] = e < a.E ? key[c][j] : -INFINITY;
+            key[0][c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
+            key[0][c][j] = e < a.E ? key[0][c][j] : -INFINITY;
             sl[c][j] = e < a.E ? a.e2s[ei] : -1;
-            gid[c][j] = e / per;
         }
     // the first 16 lanes select among all experts, the next 16 among the resident ones
-    select_row<double, EC>(a, key, [&](int e) { return s.score[e] * inv_z; }, sl, gid, sub, tok, lane & 16,
-                           lane & 16 ? a.slot : a.orig_expert, lane & 16 ? a.gate : a.orig_gate, lane < 32, 0.0);
+    const bool served = lane & 16;
+#pragma unroll
+    for (int c = 0; c < EC; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[0][c][j] = served && sl[c][j] < 0 ? -INFINITY : key[0][c][j];
+    int mine[1];
+    keep_groups<double, EC>(key[0], a, sub, 0.0);
+    pick_row<double, EC, 1>(key, a, sub, 0.0, mine);
+    store_choice<double>(a, mine[0], [&](int e) { return s.score[e] * inv_z; }, sub, tok, served, served ? a.slot : a.orig_expert,
+                         served ? a.gate : a.orig_gate, lane < 32);
+}
+
+// Whether another lane of the row holds a value within tol.
+template <int N = 1>
+__device__ __forceinline__ bool near_in_row(float v, float tol) {
+    bool near = fabsf(v - dpp<0x120 + N>(v)) <= tol;
+    if constexpr (N < 15) near |= near_in_row<N + 1>(v, tol);
+    return near;
 }
 
 template <int EC, class AT>
 __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, AT logit_at, float err, bool groups, topk_exact<EC>& s) {
-    const int lane = threadIdx.x & 63, sub = lane & 15, per = a.E / a.groups;
+    const int lane = threadIdx.x & 63, per = a.E / a.groups;
     const bool all = !a.sigmoid && !a.by_logit;
     float* fkey = (float*)s.score;
     float* rkey = fkey + 64 * EC;
@@ -280,57 +386,60 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
     for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     const float tol = 2.f * (a.by_logit ? err : 0.25f * err + 4.8e-7f * (most + 1.f));
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // lanes of a wave read what others wrote: its LDS accesses are in order
-    unsigned near_all = 0, near_res = 0;                   // groups whose rank is near another's
+    // Groups whose rank is near another's, and the least key of those that make a group's rank (lane g: group g).
+    bool near_group[2] = {false, false};
+    float made_of[2];
     if (groups) {
-        float r[2];
 #pragma unroll
         for (int res = 0; res < 2; ++res) {
             float m1 = -INFINITY, m2 = -INFINITY;
+            const float* keys = res ? rkey : fkey;
 #pragma unroll 1
-            for (int f = 0; f < per; ++f) {
-                const float v = lane < a.groups ? (res ? rkey : fkey)[lane * per + f] : -INFINITY;
-                m2 = fmaxf(m2, fminf(m1, v));
-                m1 = fmaxf(m1, v);
+            for (int f = 0; f < per; f += 4) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = keys[min(min(lane, a.groups - 1) * per + f + i, a.E - 1)];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float u = lane < a.groups && f + i < per ? v[i] : -INFINITY;
+                    m2 = fmaxf(m2, fminf(m1, u));
+                    m1 = fmaxf(m1, u);
+                }
             }
-            r[res] = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
+            made_of[res] = a.best == 2 ? m2 : m1;
+            const float rank = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
+            near_group[res] = near_in_row(rank, 2.f * tol);    // (lanes behind the groups are infinitely far)
         }
-#pragma unroll 1
-        for (int g = 0; g < a.groups; ++g) {
-            const float o0 = __shfl(r[0], g), o1 = __shfl(r[1], g);
-            near_all |= lane != g && fabsf(r[0] - o0) <= 2.f * tol;
-            near_res |= lane != g && fabsf(r[1] - o1) <= 2.f * tol;
-        }
-        near_all = (unsigned)__ballot(lane < a.groups && near_all);
-        near_res = (unsigned)__ballot(lane < a.groups && near_res);
     }
     unsigned again_of = 0;                                 // bit c: this lane's expert of chunk c
+    float mine[EC];
+    int near[EC];
+#pragma unroll
+    for (int c = 0; c < EC; ++c) {
+        mine[c] = fkey[64 * c + lane];
+        near[c] = all ? 2 : 0;
+    }
+    if (!all) {
 #pragma unroll 1
-    for (int e0 = 0; e0 < a.E; e0 += 64) {
-        const int e = e0 + lane;
-        bool again = e < a.E;
-        if (!all) {
-            const float mine = fkey[e];
-            int near = 0;
-#pragma unroll 1
-            for (int f = 0; f < a.E; f += 4) {             // itself among them; past E: infinitely far
-                const float4 o = *(const float4*)(fkey + f);
-                near += (fabsf(mine - o.x) <= tol) + (fabsf(mine - o.y) <= tol) + (fabsf(mine - o.z) <= tol) + (fabsf(mine - o.w) <= tol);
-            }
-            bool top = false;
-            if (groups && again) {
-                const int f0 = e / per * per;
-                int above = 0, above_res = 0;
-#pragma unroll 1
-                for (int f = f0; f < f0 + per; ++f) {
-                    above += fkey[f] > mine;
-                    above_res += rkey[f] > mine;
-                }
-                const int g = e / per;
-                top = ((near_all >> g & 1) && above < a.best) || ((near_res >> g & 1) && rkey[e] == mine && above_res < a.best);
-            }
-            again = again && (near > 1 || top);
+        for (int f = 0; f < a.E; f += 8) {                 // itself among them; past E: infinitely far
+            const float4 lo = *(const float4*)(fkey + f), hi = *(const float4*)(fkey + f + 4);
+            const float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int c = 0; c < EC; ++c) near[c] += fabsf(mine[c] - o[i]) <= tol;
         }
-        again_of |= (again ? 1u : 0u) << (e0 >> 6);
+    }
+#pragma unroll
+    for (int c = 0; c < EC; ++c) {
+        const int e = 64 * c + lane, g = min(group_of(a, e), a.groups - 1);
+        bool again = near[c] > 1;
+        if (groups) {
+            const bool in_all = __shfl((int)near_group[0], g), in_res = __shfl((int)near_group[1], g);
+            const float least = __shfl(made_of[0], g), least_res = __shfl(made_of[1], g);
+            again |= (in_all && mine[c] >= least) || (in_res && rkey[e] == mine[c] && mine[c] >= least_res);
+        }
+        again_of |= (again && e < a.E ? 1u : 0u) << c;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     int* list = (int*)fkey;                                // the keys have been used up
@@ -343,31 +452,49 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
         n += __popcll(m);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    // four experts at a time, 16 lanes each
+    // two experts at a time, 32 lanes each, four pieces of a row on their way together
 #pragma unroll 1
-    for (int i = lane >> 4; i < n + (lane >> 4); i += 4) {
+    for (int i = lane >> 5; i < n + (lane >> 5); i += 2) {
         const int e = list[min(i, n - 1)];
         // the expert's row: the caller's, or out of the operand order that the product has just read (there it is in the L2), a
         // unit of 4 weights at a time: step c / 16, half c % 8 / 4, lane e % 32 + 32 (c % 16 / 8)
         const float4* w = a.f32 ? (const float4*)(a.wrow + (size_t)e * a.d) : (const float4*)a.wr + (size_t)(e >> 5) * (a.d >> 4) * 128 + (e & 31);
         double sum = 0;
 #pragma unroll 1
-        for (int c = sub * 4; c < a.d; c += 64) {          // d_model is a multiple of 4
-            const float4 v = w[a.f32 ? c >> 2 : (c >> 4) * 128 + (c >> 2 & 1) * 64 + (c >> 3 & 1) * 32];
-            float4 x;
-            if (a.f32) x = *(const float4*)((const float*)a.x + (size_t)tok * a.d + c);
-            else {
-                const uint2 p = *(const uint2*)((const uint16_t*)a.x + (size_t)tok * a.d + c);
-                x = make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16),
-                                __uint_as_float(p.y & 0xFFFF0000u));
+        for (int c0 = (lane & 31) * 4; c0 < a.d; c0 += 512) {     // d_model is a multiple of 4
+            float4 v[4], x[4];
+            if (a.f32) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = min(c0 + 128 * u, a.d - 4);
+                    v[u] = w[c >> 2];
+                    x[u] = *(const float4*)((const float*)a.x + (size_t)tok * a.d + c);
+                }
+            } else {
+                uint2 p[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int c = min(c0 + 128 * u, a.d - 4);
+                    v[u] = w[(c >> 4) * 128 + (c >> 2 & 1) * 64 + (c >> 3 & 1) * 32];
+                    p[u] = *(const uint2*)((const uint16_t*)a.x + (size_t)tok * a.d + c);
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    x[u] = make_float4(__uint_as_float(p[u].x << 16), __uint_as_float(p[u].x & 0xFFFF0000u), __uint_as_float(p[u].y << 16),
+                                       __uint_as_float(p[u].y & 0xFFFF0000u));
             }
-            sum = fma((double)x.x, (double)v.x, sum);
-            sum = fma((double)x.y, (double)v.y, sum);
-            sum = fma((double)x.z, (double)v.z, sum);
-            sum = fma((double)x.w, (double)v.w, sum);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (c0 + 128 * u >= a.d) v[u] = make_float4(0, 0, 0, 0);   // past the row
+                sum = fma((double)x[u].x, (double)v[u].x, sum);
+                sum = fma((double)x[u].y, (double)v[u].y, sum);
+                sum = fma((double)x[u].z, (double)v[u].z, sum);
+                sum = fma((double)x[u].w, (double)v[u].w, sum);
+            }
         }
         sum = row_sum(sum);
-        if (sub == 0) s.logit[e] = sum;
+        sum += __shfl_xor(sum, 16);
+        if ((lane & 31) == 0) s.logit[e] = sum;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     select_exact<EC>(a, tok, s);
@@ -388,9 +515,9 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
     using X = topk_exact<EC>;
     __shared__ X s_exact[X::WAVES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 15;
-    const int tw0 = block * NTOK, per = a.E / a.groups;
+    const int tw0 = block * NTOK;
     if (tid == 0) s_n = 0;
-    int sl[EC][4], gid[EC][4];
+    int sl[EC][4];
     smoe_route_slots<NEB>(sl, a, sub);
     float bias[EC][4];
 #pragma unroll
@@ -398,12 +525,12 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int e = 64 * c + 4 * sub + j;
-            gid[c][j] = e / per;
             bias[c][j] = a.bias && e < a.E ? a.bias[e] : 0.f;
         }
     const float wnorm = *a.wnorm;
     smoe_route_meet<NEB, TB>(a.E, acc, sq, part, sqp);
 
+#pragma unroll 1
     for (int tb = 0; tb < TB; ++tb) {
         const int t = tb * SMOE_RT + wave * 4 + (lane >> 4), tok = tw0 + t;
         const float* row = part + t * LDP;
@@ -433,7 +560,7 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
         for (int q = 0; q < 2 * NS; ++q) ss += sqp[t + q * NTOK];
         const float xnorm = sqrtf(ss);
-        const float err = 0x1p-24f * (a.err_norm * xnorm * wnorm + a.err_sum * smoe_row_max(big));
+        const float err = 0x1p-24f * (a.err_norm * xnorm * wnorm + a.err_sum * __int_as_float(row_max(__float_as_int(big))));
         float top = -INFINITY, z = 1.f;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -467,16 +594,37 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const bool in = 64 * c + 4 * sub + j < a.E;
-                    const float s = a.sigmoid ? sigmoid_of(v[c][j]) : expf(v[c][j] - top) * inv_z;
+                    const float s = a.sigmoid ? sigmoid_near(v[c][j]) : expf(v[c][j] - top) * inv_z;
                     v[c][j] = in ? s + bias[c][j] : -INFINITY;
                     most = fmaxf(most, in ? fmaxf(fabsf(v[c][j]), s) : 0.f);
                 }
             // a sigmoid is off by at most a quarter of its logit's error, a share of a softmax by at most twice its own size times that; and the
-            // exponential, the quotient and the sum with the bias are rounded, each by a few units of 2^-24
-            tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + 4.8e-7f * smoe_row_max(most);
+            // exponential, the quotient and the sum with the bias are rounded: units of 2^-24, 8 of them, and of the fast sigmoid s another
+            // 1.5 (1 - s) |l|, where s (1 - s) |l| <= (|largest l| + 1/2) (largest s)
+            const float units = a.sigmoid ? 8.f + 2.f * fabsf(top) : 8.f;
+            tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + 0x1p-24f * units * __int_as_float(row_max(__float_as_int(most)));
         }
-        int close = select_row<float, EC>(a, v, score_at, sl, gid, sub, tok, false, a.orig_expert, a.orig_gate, tok < a.T, 2.f * tol);
-        close |= select_row<float, EC>(a, v, score_at, sl, gid, sub, tok, true, a.slot, a.gate, tok < a.T, 2.f * tol);
+        // both selections at once, or one after the other where the registers do not reach
+        constexpr int R = EC <= 2 ? 2 : 1;
+        int close = 0;
+#pragma unroll 1
+        for (int first = 0; first < 2; first += R) {
+            int key[R][EC][4], mine[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int c = 0; c < EC; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) key[r][c][j] = to_ordered(first + r && sl[c][j] < 0 ? -INFINITY : v[c][j]);
+                if (a.groups > 1) close |= keep_groups<float, EC>(key[r], a, sub, 2.f * tol);
+            }
+            close |= pick_row<float, EC, R>(key, a, sub, 2.f * tol, mine);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool served = first + r;
+                store_choice<float>(a, mine[r], score_at, sub, tok, served, served ? a.slot : a.orig_expert, served ? a.gate : a.orig_gate, tok < a.T);
+            }
+        }
         if (sub < a.k && tok < a.T) a.xnorm[(size_t)tok * a.k + sub] = xnorm;
         if (close && sub == 0 && tok < a.T) {
             const int i = atomicAdd(&s_n, 1);              // the order does not matter
@@ -650,6 +798,7 @@ int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, cons
     a.by_logit = !bias && (rule.groups == 1 || rule.group_best == 1);
     a.f32 = c.dtype == SMOE_F32;
     const int per = c.E / rule.groups;
+    a.inv_per = 1.f / per;
     a.aligned = per >= 4 && per <= 64 && !(per & (per - 1));
     // The partial sums of a logit pass through n roundings.  Where x points nowhere in particular they are small, and the error measured at
     // most 0.75 |x| |w| 2^-24 (bf16; fp32: 1.3) in batches of 16384 tokens, 64 .. 16384 columns and up to 256 experts.  Where x follows a row of the
