@@ -557,12 +557,17 @@ __global__ __launch_bounds__(256) void scatter_rows_kernel(const uint4* __restri
     }
 }
 
+// Up to here the launches of permute_rows_kernel, as for single choices, beyond those of the ranks and the rows: a block's share of the histograms
+// costs more in every one of so many workgroups than a launch.  4 pairs a token, 32 slots, rows of 2 KB (us, rows' kernel / ranks and rows): 2800 pairs
+// 10.0 / 10.4, 4096 10.4 / 10.4, 8192 13.2 / 10.8, 16384 17.9 / 13.4, 28000 24.5 / 17.3, 65536 73 / 39; 28000 of 1 KB 21.4 / 12.5.
+constexpr int PAIRS_TWO_MAX = 4096;
+
 int launch_permute_pairs(const smoe_config& c, const void* x, const int32_t* slot, int T, int k, void* x_perm, int32_t* perm,
                          int32_t* inv_perm, int32_t* offsets, int32_t* hist, hipStream_t s) {
     const int n = T * k, K = c.K, cpr = (int)((size_t)c.d_model * smoe_elem_size(c.dtype) / 16), nblk = smoe_sort_blocks(n);
     if (n <= PERM_ONE_MAX) hist = nullptr;
     else hipLaunchKernelGGL(sort_hist_kernel, dim3(nblk), dim3(SB), K * sizeof(int32_t), s, slot, n, K, hist);
-    if (permute_fused(c, n) || (!x_perm && n <= PERM_TWO_MAX)) {
+    if (n <= PAIRS_TWO_MAX) {
         const int parts = cpr >= 256 && n <= PERM_WIDE_MAX ? 16 : 4;
         const int blocks = std::max(1, (n + 63) / 64);     // an empty batch still writes offsets = 0
         hipLaunchKernelGGL((parts == 16 ? permute_rows_kernel<16, true> : permute_rows_kernel<4, true>), dim3(parts * blocks), dim3(256), 0, s,
