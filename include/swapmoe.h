@@ -345,6 +345,8 @@ int smoe_add_norm(smoe_layer_t* layer, const void* x, const void* residual, cons
  *           ids; a group ranks by the sum of its group_best (1 or 2) largest values,
  *           the groups_kept best groups stay, and among their experts the k
  *           largest values are chosen, best first (lower id, lower group on a tie)
+ *           (without a bias, where single values rank the groups or there is one, the
+ *           logits themselves are compared: scores that round to 1 are no tie)
  *   weight  s, without the bias; divided by the sum over the chosen experts with
  *           renorm = 1; times scale
  * Limits: k <= 16, groups <= 16 and a divisor of E, k <= the experts of
