@@ -68,7 +68,7 @@ smoe_ws_layout smoe_ws_plan(const smoe_config& c) {
     const size_t rows = std::max((size_t)c.max_tokens + 32 * (size_t)c.K, smoe_small_batch_rows(c));
     const size_t hidden = c.dtype == SMOE_MXFP8 ? smoe_mx_hidden_bytes(c) : rows * c.d_ff * smoe_elem_size(c.dtype);
     // (in front of a pass's products, smoe_route_topk keeps the logits of few tokens there)
-    const size_t logits64 = (size_t)std::min(c.max_tokens, SMOE_TOPK_FEW) * c.E * 8;
+    const size_t logits64 = (size_t)std::min(c.max_tokens, smoe_topk_few_tokens(c.dtype)) * c.E * 8;
     w.hidden = off;  off = align_up(off + std::max(hidden, logits64), 256);
     // bf16 activations: the router's weights in matrix-operand order, experts padded to a multiple of 32
     w.rsplit = off;

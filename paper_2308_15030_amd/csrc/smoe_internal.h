@@ -147,7 +147,8 @@ inline size_t smoe_scale_pitch(int d) { return ((size_t)d / 32 + 7) / 8 * 8; }  
 // whose rows (8 elements of padding each) fit the dynamic LDS of a compute unit; the path keeps the hidden
 // activations of every slot for every token of the batch, in blocks of 32 tokens.
 constexpr int SMOE_SMALL_T = 128;
-constexpr int SMOE_TOPK_FEW = 128;                         // most tokens of smoe_route_topk's launches for few tokens
+// Most tokens of smoe_route_topk's launches for few tokens (see topk_few in route_topk.hip).
+inline int smoe_topk_few_tokens(int dtype) { return dtype == SMOE_F32 ? 512 : 128; }
 constexpr int SMOE_FEW_T = 16;                             // ... and at most this many take its launches for few tokens
 constexpr int SMOE_SMALL_LDS = 160 * 1024 - 2048;          // the rest covers the static tables
 inline size_t smoe_small_batch_rows(const smoe_config& c) {

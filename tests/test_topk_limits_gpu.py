@@ -107,3 +107,17 @@ def test_events_take_the_products_times(T):
         assert torch.equal(L.y_perm, plain)
         assert 0 < ev[0].elapsed_time(ev[1]) < 100 and 0 < ev[2].elapsed_time(ev[3]) < 100
     L.close()
+
+
+@pytest.mark.parametrize("E,d,T,dtype", [(33, 100, 511, b.SMOE_F32), (33, 100, 512, b.SMOE_F32), (33, 100, 513, b.SMOE_F32), (64, 1024, 128, b.SMOE_BF16),
+                                         (64, 1024, 129, b.SMOE_BF16), (64, 992, 128, b.SMOE_BF16), (129, 512, 127, b.SMOE_MXFP8)])
+def test_route_where_the_launches_change(E, d, T, dtype):
+    """Few tokens take two launches, more of them one: both sides of the borders, against float64."""
+    from test_topk_gpu import _check_route, _route_case, layer
+    K, k = E // 3, 4
+    router, x, resident, g = _route_case(E, K, d, T, dtype, E + T, 0.05)
+    L = layer(E, K, d, T * k + 3, dtype, router, resident)
+    bias = (0.05 * torch.randn(E, generator=g)).to(DEV)
+    _check_route(L, x.to(DEV), T, b.smoe_topk_rule(k, b.SMOE_SCORE_SIGMOID, renorm=0), bias, router, resident, dtype)
+    _check_route(L, x.to(DEV), T, b.smoe_topk_rule(k), None, router, resident, dtype)
+    L.close()
