@@ -9,8 +9,8 @@
 // Two forms of each product:
 //   stream_mx_kernel   few rows a slot: what bounds it is the bytes of the weights.  A wave takes one block of 32 features and a
 //                      share of the reduction, several loads ahead, straight into registers.
-//   tile_mx_kernel     many rows a slot: the matrix cores bound it.  Weights go straight into registers (no other wave of the
-//                      workgroup needs them), the token tile is staged through LDS.
+//   tile_mx_kernel     many rows a slot: what bounds it is the way of the operands through LDS next to the matrix cores.  Both are staged
+//                      there, 16384 rows of 1024 x 4096: 1460 TFLOP/s.
 
 #include <algorithm>
 #include <climits>
@@ -235,7 +235,8 @@ __global__ __launch_bounds__(64 * NW) void stream_mx_kernel(const MxArgs g) {
 // Two workgroups to a compute unit (FB = 8: 80 KB of LDS each), so that one multiplies while the other waits at its barrier, looks its next tile up
 // or narrows its results.  A workgroup of 256 x 256 tiles with twice the accumulators moves a third fewer bytes a product, but its waves are alone on
 // their SIMDs: 239 us for the 16384 rows of 1024 x 4096 that take 190 here, 210 with its next tile's loads in flight through the stores.  Traces of copies
-// without a part (one slot, first + second product, 171 us): without loads 140, without products 143, without stores 133.
+// without a part (one slot, first + second product, 171 us): without loads 140, without products 143, without stores 133; second product of 4 slots, 92
+// us: without loads 68, also without operand reads 55, without loads and products 56, barriers and stores alone 25.
 extern __shared__ __align__(16) char mx_lds[];
 constexpr int MX_BLK = 2048;              // bytes of a block of one step
 constexpr int TILE_COST0 = 20;            // a tile beside its steps, in steps of one token block; 0 to 60 chose tiles of the same speed
@@ -455,7 +456,8 @@ __global__ __launch_bounds__(256, FB == 8 ? 2 : 3) void tile_mx_kernel(const MxA
         for (int a = 0; a < AW; ++a)
 #pragma unroll
             for (int b = 0; b < NBW; ++b)
-                if (b == 0 || b * WT + wt < nb) smoe_mx_mfma<u>(acc[a][b], wv[a], tv[b], ws[a], ts[b]);
+                if (b == 0 || b * WT + wt < nb)            // (without the branch, all products in a row: 99 us for 91)
+                    smoe_mx_mfma<u>(acc[a][b], wv[a], tv[b], ws[a], ts[b]);
         cst = cst == (ST - 1) * S::STAGE ? 0 : cst + S::STAGE;
     };
     // Step c + 1 has landed: what may be outstanding are the loads of the ST - 2 steps behind it.
