@@ -300,7 +300,7 @@ __device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, 
 }
 
 // One token again in 64 bits, by one wave.  Only logits whose order is in question are computed again: those of experts whose keys are within
-// the tolerance of another's, those that rank a group near another where the groups are in question (`groups`), all of them where a bias meets the softmax (every key holds the sum over all).
+// the tolerance of another's, and those that rank a group near another where the groups are in question (`groups`).
 // The others keep their fp32 logits, which are apart from whatever they are compared with.  Few tokens come here, and a workgroup that has one is
 // the last to end, so what counts is the time of one pass: 27000 cycles with two logits to repeat (16384 tokens, 8 of 128 experts: 11 of 53 us), of
 // which 1500 for the keys, 500 for the groups, 5300 for the distances, 3900 for the products and 14000 for the selection, whose code comes from memory
@@ -370,14 +370,13 @@ __device__ __forceinline__ bool near_in_row(float v, float tol) {
 template <int EC, class AT>
 __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, AT logit_at, float err, bool groups, topk_exact<EC>& s) {
     const int lane = threadIdx.x & 63, per = a.E / a.groups;
-    const bool all = !a.sigmoid && !a.by_logit;
     float* fkey = (float*)s.score;
     float* rkey = fkey + 64 * EC;
     float most = 0.f;
 #pragma unroll 1
     for (int e = lane; e < 64 * EC; e += 64) {
         const float l = e < a.E ? logit_at(e) : -INFINITY;
-        const float key = a.by_logit || all || e >= a.E ? l : sigmoid_of(l) + (a.bias ? a.bias[e] : 0.f);
+        const float key = a.by_logit || e >= a.E ? l : sigmoid_of(l) + (a.bias ? a.bias[e] : 0.f);
         s.logit[e] = l;
         fkey[e] = key;
         rkey[e] = e < a.E && a.e2s[e] >= 0 ? key : -INFINITY;
@@ -417,18 +416,16 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
 #pragma unroll
     for (int c = 0; c < EC; ++c) {
         mine[c] = fkey[64 * c + lane];
-        near[c] = all ? 2 : 0;
+        near[c] = 0;
     }
-    if (!all) {
 #pragma unroll 1
-        for (int f = 0; f < a.E; f += 8) {                 // itself among them; past E: infinitely far
-            const float4 lo = *(const float4*)(fkey + f), hi = *(const float4*)(fkey + f + 4);
-            const float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    for (int f = 0; f < a.E; f += 8) {                 // itself among them; past E: infinitely far
+        const float4 lo = *(const float4*)(fkey + f), hi = *(const float4*)(fkey + f + 4);
+        const float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int c = 0; c < EC; ++c) near[c] += fabsf(mine[c] - o[i]) <= tol;
-        }
+            for (int c = 0; c < EC; ++c) near[c] += fabsf(mine[c] - o[i]) <= tol;
     }
 #pragma unroll
     for (int c = 0; c < EC; ++c) {
@@ -498,6 +495,50 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     select_exact<EC>(a, tok, s);
+}
+
+__device__ __forceinline__ float4 load_x4(const smoe_topk_args& a, size_t at) {
+    if (a.f32) return *(const float4*)((const float*)a.x + at);
+    const uint2 p = *(const uint2*)((const uint16_t*)a.x + at);
+    return make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xFFFF0000u));
+}
+
+// Where a bias meets the softmax every key holds the sum over all experts, and all logits are computed again: lane l's are those of the experts
+// 64 c + l, over the columns 4 q0 .. 4 q1 - 1.
+template <int EC>
+__device__ __forceinline__ void all_logits(const smoe_topk_args& a, int tok, int q0, int q1, double (&sum)[EC]) {
+    const int lane = threadIdx.x & 63;
+    const float4* w[EC];
+#pragma unroll
+    for (int c = 0; c < EC; ++c) {
+        const int e = min(64 * c + lane, a.E - 1);
+        w[c] = a.f32 ? (const float4*)(a.wrow + (size_t)e * a.d) : (const float4*)a.wr + (size_t)(e >> 5) * (a.d >> 4) * 128 + (e & 31);
+        sum[c] = 0;
+    }
+    constexpr int U = 4;                                   // on their way together
+#pragma unroll 1
+    for (int q = q0; q < q1; q += U) {
+        float4 v[EC][U], x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int qq = min(q + u, q1 - 1), at = a.f32 ? qq : (qq >> 2) * 128 + (qq & 1) * 64 + (qq >> 1 & 1) * 32;
+            x[u] = load_x4(a, (size_t)tok * a.d + 4 * qq);
+#pragma unroll
+            for (int c = 0; c < EC; ++c) v[c][u] = w[c][at];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (q + u >= q1) x[u] = make_float4(0, 0, 0, 0);   // past the columns
+            const double x0 = x[u].x, x1 = x[u].y, x2 = x[u].z, x3 = x[u].w;
+#pragma unroll
+            for (int c = 0; c < EC; ++c) {
+                sum[c] = fma(x0, (double)v[c][u].x, sum[c]);
+                sum[c] = fma(x1, (double)v[c][u].y, sum[c]);
+                sum[c] = fma(x2, (double)v[c][u].z, sum[c]);
+                sum[c] = fma(x3, (double)v[c][u].w, sum[c]);
+            }
+        }
+    }
 }
 
 }  // namespace
@@ -634,6 +675,45 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
     }
     __syncthreads();
     const int n = s_n;
+    if (!a.sigmoid && !a.by_logit) {
+        const int quads = a.d >> 2;
+        double sum[EC];
+        if (n <= 2) {                                      // (uniform) the whole workgroup on one token, a share of the columns each
+            constexpr int W = X::WAVES;
+            const int share = (quads + W - 1) / W;
+            for (int i = 0; i < n; ++i) {
+                const int tok = tw0 + (__builtin_amdgcn_readfirstlane(s_close[i]) & 255);
+                if (wave < W) {
+                    all_logits<EC>(a, tok, min(wave * share, quads), min((wave + 1) * share, quads), sum);
+#pragma unroll
+                    for (int c = 0; c < EC; ++c) s_exact[wave].logit[64 * c + lane] = sum[c];
+                }
+                __syncthreads();
+                if (wave == 0) {
+#pragma unroll
+                    for (int c = 0; c < EC; ++c) {
+                        double v = 0;
+                        for (int w = 0; w < W; ++w) v += s_exact[w].logit[64 * c + lane];   // fixed order
+                        s_exact[0].logit[64 * c + lane] = v;
+                    }
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    select_exact<EC>(a, tok, s_exact[0]);
+                }
+                __syncthreads();
+            }
+            return;
+        }
+        if (wave >= X::WAVES) return;
+        for (int i = wave; i < n; i += X::WAVES) {         // a wave each
+            const int tok = tw0 + (__builtin_amdgcn_readfirstlane(s_close[i]) & 255);
+            all_logits<EC>(a, tok, 0, quads, sum);
+#pragma unroll
+            for (int c = 0; c < EC; ++c) s_exact[wave].logit[64 * c + lane] = sum[c];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            select_exact<EC>(a, tok, s_exact[wave]);
+        }
+        return;
+    }
     if (wave >= X::WAVES) return;
     for (int i = wave; i < n; i += X::WAVES) {             // a wave each
         const int word = __builtin_amdgcn_readfirstlane(s_close[i]), t = word & 255;
@@ -696,12 +776,6 @@ int launch(const smoe_topk_args& a, hipStream_t s) {
 // Few tokens: a workgroup of the kernels above would read the whole router alone.  Here a wave takes the product of one expert with FEW_TOK tokens, in
 // 64 bits (so that nothing has to be repeated), and a second launch selects, a wave a token.
 constexpr int FEW_TOK = 4;
-
-__device__ __forceinline__ float4 load_x4(const smoe_topk_args& a, size_t at) {
-    if (a.f32) return *(const float4*)((const float*)a.x + at);
-    const uint2 p = *(const uint2*)((const uint16_t*)a.x + at);
-    return make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xFFFF0000u));
-}
 
 __global__ __launch_bounds__(256) void topk_logits_kernel(const smoe_topk_args a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
