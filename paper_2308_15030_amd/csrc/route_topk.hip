@@ -280,17 +280,30 @@ __device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC
     return close;
 }
 
-// What lane `sub` has chosen: weight and identity, among the resident experts with `served`, else among all.  score_at: an expert's score.  store: write
-// the results to id and gate.
-template <class T, class AT>
-__device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, AT score_at, int sub, int tok, bool served, int32_t* id, float* gate,
-                                             bool store) {
+__device__ __forceinline__ float exp_of(float v) { return expf(v); }
+__device__ __forceinline__ double exp_of(double v) { return exp(v); }
+
+// What lane `sub` has chosen: weight and identity, among the resident experts with `served`, else among all.  score_at, logit_at: an expert's score and
+// logit.  store: write the results to id and gate.
+// Weights that are divided by their sum are taken in units of e^m, m the largest exponent among the chosen, which cancels: e^(l - m) for a softmax,
+// e^(min(l, 0) - m) / (1 + e^-|l|) for a sigmoid.  The scores themselves may all be zero: those of residents more than 104 below the best of all experts are in
+// fp32.
+template <class T, class SCORE, class LOGIT>
+__device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, SCORE score_at, LOGIT logit_at, int sub, int tok, bool served, int32_t* id,
+                                             float* gate, bool store) {
     const int e = min(max(mine, 0), a.E - 1);
     T w = 0;
-    if (mine >= 0) w = score_at(e);
     if (a.renorm) {
+        const T l = mine >= 0 ? T(logit_at(e)) : T(-INFINITY), p = a.sigmoid ? smaller(l, T(0)) : l;
+        const T m = row_max(p);
+        if (mine >= 0) {
+            w = exp_of(p - m);
+            if (a.sigmoid) w /= 1 + exp_of(l < 0 ? l : -l);
+        }
         const T sum = row_sum(w);
         w = sum > 0 ? w / sum : T(0);
+    } else if (mine >= 0) {
+        w = score_at(e);
     }
     if (sub < a.k && store) {
         const size_t at = (size_t)tok * a.k + sub;
@@ -355,8 +368,8 @@ __device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, t
     int mine[1];
     keep_groups<double, EC>(key[0], a, sub, 0.0);
     pick_row<double, EC, 1>(key, a, sub, 0.0, mine);
-    store_choice<double>(a, mine[0], [&](int e) { return s.score[e] * inv_z; }, sub, tok, served, served ? a.slot : a.orig_expert,
-                         served ? a.gate : a.orig_gate, lane < 32);
+    store_choice<double>(a, mine[0], [&](int e) { return s.score[e] * inv_z; }, [&](int e) { return s.logit[e]; }, sub, tok, served,
+                         served ? a.slot : a.orig_expert, served ? a.gate : a.orig_gate, lane < 32);
 }
 
 // Whether another lane of the row holds a value within tol.
@@ -663,7 +676,8 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const bool served = first + r;
-                store_choice<float>(a, mine[r], score_at, sub, tok, served, served ? a.slot : a.orig_expert, served ? a.gate : a.orig_gate, tok < a.T);
+                store_choice<float>(a, mine[r], score_at, logit_at, sub, tok, served, served ? a.slot : a.orig_expert, served ? a.gate : a.orig_gate,
+                                    tok < a.T);
             }
         }
         if (sub < a.k && tok < a.T) a.xnorm[(size_t)tok * a.k + sub] = xnorm;
