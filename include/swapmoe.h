@@ -392,7 +392,8 @@ int smoe_permute_topk(smoe_layer_t* layer, const void* x, const int32_t* slot, i
  * bank to blocks of 32 consecutive elements of a column (along the reduction), and h rounded
  * to blocks of 32 features between the products; products and sums on the
  * matrix cores in fp32, y_perm bf16, rounded once.  Rows from offsets[K] on are
- * left as they were. */
+ * left as they were.  A row with a NaN among its values becomes NaN throughout;
+ * other rows' bits do not depend on it. */
 int smoe_expert_ffn_mx(smoe_layer_t* layer, const void* q, const void* q_scale, const int32_t* perm, int k,
                        const int32_t* offsets, int T, void* y_perm, void* stream);
 

@@ -56,7 +56,7 @@ __device__ __forceinline__ void store_hidden(const MxArgs& g, f32x16& acc, int r
     float amax = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        acc[i] = fmaxf(acc[i], 0.f);
+        acc[i] = __builtin_elementwise_maximum(acc[i], 0.f);   // (keeps a NaN, as fmaxf does not)
         amax = fmaxf(amax, acc[i]);
     }
     uint32_t lo = __float_as_uint(amax), hi = lo;
