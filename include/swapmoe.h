@@ -369,7 +369,9 @@ typedef struct {
  * gate_mode plays no part.  Choices nearer to one another than the error of an
  * fp32 logit are decided again in 64 bits.  The first call after a bind
  * prepares the router's weights in the workspace; router_w must still hold them at
- * later calls.  SMOE_ESTATE until every slot has been filled. */
+ * later calls.  A token with a NaN takes experts like any other, those whose logits are NaN
+ * behind the others in the order of their ids, and their weights are NaN.
+ * SMOE_ESTATE until every slot has been filled. */
 int smoe_route_topk(smoe_layer_t* layer, const smoe_topk_rule* rule /*host*/, const float* bias, const void* x,
                     int T, int32_t* orig_expert, float* orig_gate, int32_t* slot, float* gate, float* xnorm,
                     void* stream);

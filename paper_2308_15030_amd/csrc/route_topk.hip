@@ -13,6 +13,7 @@
 // Without a bias, and with single experts ranking the groups, the keys are the logits themselves, of which every score is a rising
 // function.
 
+#include <cfloat>
 #include <climits>
 
 #include "route_mfma.h"
@@ -90,10 +91,17 @@ __device__ __forceinline__ void row_min(int (&v)[R]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) v[r] = min(v[r], dpp<0x121>(v[r]));
 }
-// Integers in the order of the floats, and back; a float that is no number becomes -infinity.
+// Integers in the order of the floats, and back (of floats that are numbers).
 __device__ __forceinline__ int ordered_bits(int i) { return i ^ (i >> 31 & 0x7fffffff); }
-__device__ __forceinline__ int to_ordered(float v) { return ordered_bits(__float_as_int(fmaxf(v, -INFINITY))); }
+__device__ __forceinline__ int to_ordered(float v) { return ordered_bits(__float_as_int(v)); }
 __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(ordered_bits(i)); }
+// The key of an expert whose logit is NaN: behind all numbers, in front of what cannot be had (-infinity).  Sums of two such keys are kept from
+// becoming -infinity.
+__device__ __forceinline__ float last_key(float) { return -FLT_MAX; }
+__device__ __forceinline__ double last_key(double) { return -1e300; }
+template <class T>
+__device__ __forceinline__ T number_or_last(T v) { return v == v ? v : last_key(v); }
+
 // What keys are compared as: floats as integers in their order, doubles as they are.
 template <class T>
 struct key_order {
@@ -146,7 +154,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             if (lanes >= 4) merge(dpp<0x4E>(m1), dpp<0x4E>(m2));
             if (lanes >= 8) merge(dpp<0x141>(m1), dpp<0x141>(m2));   // the other quad of eight lanes
             if (lanes >= 16) merge(dpp<0x140>(m1), dpp<0x140>(m2));  // the other eight
-            rank[c] = a.best == 2 && m2 > none ? O::of(O::value(m1) + O::value(m2)) : m1;
+            rank[c] = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
         }
         int ahead[EC];
 #pragma unroll
@@ -200,7 +208,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             merge(dpp<0x124>(m1), dpp<0x124>(m2));
             merge(dpp<0x122>(m1), dpp<0x122>(m2));
             merge(dpp<0x121>(m1), dpp<0x121>(m2));
-            const I r = a.best == 2 && m2 > none ? O::of(O::value(m1) + O::value(m2)) : m1;
+            const I r = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
             rank = g == sub ? r : rank;
         }
         unsigned kept = 0;
@@ -300,14 +308,14 @@ __device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, 
             w = exp_of(p - m);
             if (a.sigmoid) w /= 1 + exp_of(l < 0 ? l : -l);
         }
-        const T sum = row_sum(w);
-        w = sum > 0 ? w / sum : T(0);
+        const T sum = row_sum(w);                          // at least 1/2
+        if (mine >= 0) w /= sum;
     } else if (mine >= 0) {
         w = score_at(e);
     }
     if (sub < a.k && store) {
         const size_t at = (size_t)tok * a.k + sub;
-        id[at] = !served ? e : mine < 0 ? -1 : a.e2s[e];   // (a token whose logits are all NaN: expert 0, weight 0)
+        id[at] = !served ? e : mine < 0 ? -1 : a.e2s[e];
         gate[at] = (float)(w * a.scale);
     }
 }
@@ -356,7 +364,7 @@ __device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, t
         for (int j = 0; j < 4; ++j) {
             const int e = 64 * c + 4 * sub + j, ei = min(e, a.E - 1);
             key[0][c][j] = a.by_logit ? s.logit[ei] : s.score[ei] * inv_z + (a.bias ? (double)a.bias[ei] : 0.0);
-            key[0][c][j] = e < a.E ? key[0][c][j] : -INFINITY;
+            key[0][c][j] = e < a.E ? number_or_last(key[0][c][j]) : -INFINITY;
             sl[c][j] = e < a.E ? a.e2s[ei] : -1;
         }
     // the first 16 lanes select among all experts, the next 16 among the resident ones
@@ -658,6 +666,10 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             const float units = a.sigmoid ? 8.f + 2.f * fabsf(top) : 8.f;
             tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + 0x1p-24f * units * __int_as_float(row_max(__float_as_int(most)));
         }
+#pragma unroll
+        for (int c = 0; c < EC; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[c][j] = number_or_last(v[c][j]);
         // both selections at once, or one after the other where the registers do not reach
         constexpr int R = EC <= 2 ? 2 : 1;
         int close = 0;
