@@ -183,8 +183,9 @@ int smoe_policy_scores(int policy, int E, const int32_t* count /*host*/, const f
  * slots not used by this batch, least recently used first (ties: lower slot),
  * until either list ends.  The pairs are written to changed_slots /
  * changed_experts (host, capacity K) and their number is returned; the caller
- * loads them with smoe_set_resident.  The use stamps live in the handle and
- * start afresh at smoe_bind. */
+ * loads them with smoe_set_resident.  An entry of -1 asks for nothing
+ * (smoe_route_topk).  The use stamps live in the handle and start afresh at
+ * smoe_bind. */
 int smoe_on_demand_plan(smoe_layer_t* layer, const int32_t* orig_expert /*host*/, int T,
                         int32_t* changed_slots /*host*/, int32_t* changed_experts /*host*/);
 
@@ -359,7 +360,9 @@ typedef struct {
 
 /* Router and Masked Gating for k experts per token.  x [T, d_model], bias [E]
  * fp32 or NULL.  For every token, with choices in order:
- *   orig_expert, orig_gate [T, k]  the rule applied to all experts
+ *   orig_expert, orig_gate [T, k]  the rule applied to all experts; an expert whose bias is
+ *       -infinity cannot be had, and where fewer than k can, the rest is expert -1, gate 0,
+ *       which smoe_importance and smoe_on_demand_plan pass over
  *   slot, gate [T, k]              the rule applied to the resident experts alone: a
  *       group of which none is resident is not kept, one with a single resident
  *       expert ranks by that one; where fewer than k can be had, the rest is

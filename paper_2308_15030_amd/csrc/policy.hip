@@ -41,6 +41,7 @@ int smoe_on_demand_plan(smoe_layer_t* L, const int32_t* orig_expert, int T, int3
     std::vector<int> wanted(E, 0);
     for (int t = 0; t < T; ++t) {
         const int e = orig_expert[t];
+        if (e == -1) continue;                       // a choice that could not be had (smoe_route_topk)
         if (e < 0 || e >= E) return smoe_fail(SMOE_EINVAL, "smoe_on_demand_plan: orig_expert[%d] = %d outside [0,%d)", t, e, E);
         const int s = L->expert_to_slot[e];
         if (s >= 0) L->last_use[s] = now;           // a hit: the slot was used by this batch

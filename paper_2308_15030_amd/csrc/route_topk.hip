@@ -315,7 +315,7 @@ __device__ __forceinline__ void store_choice(const smoe_topk_args& a, int mine, 
     }
     if (sub < a.k && store) {
         const size_t at = (size_t)tok * a.k + sub;
-        id[at] = !served ? e : mine < 0 ? -1 : a.e2s[e];
+        id[at] = mine < 0 ? -1 : served ? a.e2s[e] : e;
         gate[at] = (float)(w * a.scale);
     }
 }
