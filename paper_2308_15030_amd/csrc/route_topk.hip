@@ -15,6 +15,7 @@
 
 #include <cfloat>
 #include <climits>
+#include <type_traits>
 
 #include "route_mfma.h"
 
@@ -127,10 +128,24 @@ __device__ __forceinline__ T row_sum(T v) {
 // e / (E / groups): e + 1/2 is at least 1/(2 per) from the next border, far more than the product's rounding
 __device__ __forceinline__ int group_of(const smoe_topk_args& a, int e) { return (int)(((float)e + 0.5f) * a.inv_per); }
 
-// The groups a token keeps, in its 16 lanes: the keys of all other experts become none.  Returns 2 where that was decided by a distance of at most
-// tol (twice that between sums of two).
+// How far keys may be off: by `base`, and by `rel` of themselves.  The second part is the rounding of a score's sum with its bias, so a bias that is large
+// counts where its own key is compared and nowhere else.
+struct key_error {
+    float base, rel;
+};
+constexpr float HALF_STEP = 0x1p-24f;
+
+// How far the rank of a group may be off, from its largest keys (best = 1: the first alone); 0 where the group has none.
+__device__ __forceinline__ float rank_error(const smoe_topk_args& a, float m1, float m2, float rank, key_error err) {
+    const float one = err.base + err.rel * fabsf(m1), two = one + err.base + err.rel * fabsf(m2) + HALF_STEP * fabsf(rank);
+    return rank == -INFINITY ? 0.f : a.best == 2 && m2 > -INFINITY ? two : one;
+}
+
+// The groups a token keeps, in its 16 lanes: the keys of all other experts become none.  Returns 2 where a group that is kept and one that is not may
+// lie the other way round (fp32 keys; in 64 bits nothing is asked).
 template <class T, int EC>
-__device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC][4], const smoe_topk_args& a, int sub, T tol) {
+__device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC][4], const smoe_topk_args& a, int sub, key_error err) {
+    constexpr bool ASK = std::is_same<T, float>::value;
     using O = key_order<T>;
     using I = typename O::type;
     const I none = O::of(-INFINITY);
@@ -140,6 +155,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
         // own groups with the steps of one reduction, and counts the groups in front of each (16384 tokens, 8 groups of 16: 18 us
         // less than the walk over the groups below).
         I rank[EC];
+        float off[EC];
         const int lanes = a.E / a.groups >> 2;
 #pragma unroll
         for (int c = 0; c < EC; ++c) {
@@ -155,6 +171,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             if (lanes >= 8) merge(dpp<0x141>(m1), dpp<0x141>(m2));   // the other quad of eight lanes
             if (lanes >= 16) merge(dpp<0x140>(m1), dpp<0x140>(m2));  // the other eight
             rank[c] = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
+            if constexpr (ASK) off[c] = rank_error(a, O::value(m1), O::value(m2), O::value(rank[c]), err);
         }
         int ahead[EC];
 #pragma unroll
@@ -171,20 +188,26 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
                 }
             }
         }
-        I worst = O::of(T(INFINITY)), next = none;
+        float worst = INFINITY, next = -INFINITY;          // least that a kept group may have, most that another may
 #pragma unroll
         for (int c = 0; c < EC; ++c) {
             if (64 * c >= a.E) continue;                   // uniform
-            const bool in = 64 * c + 4 * sub < a.E;
-            const bool keep = in && ahead[c] < a.kept && rank[c] > none;
-            worst = smaller(worst, in && ahead[c] < a.kept ? rank[c] : O::of(T(INFINITY)));
-            next = larger(next, in && ahead[c] >= a.kept ? rank[c] : none);
+            const bool in = 64 * c + 4 * sub < a.E, before = ahead[c] < a.kept;
+            const bool keep = in && before && rank[c] > none;
+            if constexpr (ASK) {
+                worst = fminf(worst, in && before ? O::value(rank[c]) - off[c] : INFINITY);
+                next = fmaxf(next, in && !before ? O::value(rank[c]) + off[c] : -INFINITY);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) key[c][j] = keep ? key[c][j] : none;
         }
-        close = O::value(row_min(worst)) - O::value(row_max(next)) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;   // (two empty groups: NaN, not close)
+        if constexpr (ASK) {
+            next = row_max(next);
+            close = row_min(worst) <= next && next > -INFINITY ? 2 : 0;
+        }
     } else if (a.groups > 1) {
         I rank = none;                                     // of group `sub`
+        float off = 0.f;
         int gid[EC][4];
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -210,16 +233,21 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             merge(dpp<0x121>(m1), dpp<0x121>(m2));
             const I r = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
             rank = g == sub ? r : rank;
+            if constexpr (ASK) off = g == sub ? rank_error(a, O::value(m1), O::value(m2), O::value(r), err) : off;
         }
         unsigned kept = 0;
-        I last = O::of(T(INFINITY));
+        I left = rank;
         for (int i = 0; i < a.kept; ++i) {
-            last = row_max(rank);
-            const int w = row_min(rank == last ? sub : 99);
-            if (last > none) kept |= 1u << (w & 31);
-            rank = w == sub ? none : rank;
+            const I most = row_max(left);
+            const int w = row_min(left == most ? sub : 99);
+            if (most > none) kept |= 1u << (w & 31);
+            left = w == sub ? none : left;
         }
-        close = O::value(last) - O::value(row_max(rank)) <= (a.best == 2 ? 2 * tol : tol) ? 2 : 0;
+        if constexpr (ASK) {
+            const bool mine = kept >> sub & 1u;
+            const float worst = row_min(mine ? O::value(rank) - off : INFINITY), next = row_max(mine ? -INFINITY : O::value(rank) + off);
+            close = worst <= next && next > -INFINITY ? 2 : 0;
+        }
 #pragma unroll
         for (int c = 0; c < EC; ++c)
 #pragma unroll
@@ -229,18 +257,20 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
 }
 
 // The best experts by key of one token, in its 16 lanes, of R lists of keys at once (one's steps fill the other's waits): lane `sub` is left with
-// choice number `sub` of each in `mine` (-1: none).  Returns whether a choice was decided by a distance of at most tol.
+// choice number `sub` of each in `mine` (-1: none).  Returns whether two that follow each other may lie the other way round (fp32 keys).
 template <class T, int EC, int R>
-__device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC][4], const smoe_topk_args& a, int sub, T tol, int (&mine)[R]) {
+__device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC][4], const smoe_topk_args& a, int sub, key_error err, int (&mine)[R]) {
+    constexpr bool ASK = std::is_same<T, float>::value;
     using O = key_order<T>;
     using I = typename O::type;
     const I none = O::of(-INFINITY);
     int close = 0;
-    T last[R];
+    float last[R], reach[R];                               // the choice before, and both errors where the next is near it
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         mine[r] = -1;
         last[r] = INFINITY;
+        reach[r] = -1.f;                                   // the first is near nothing
     }
 #pragma unroll 1
     for (int i = 0; i <= a.k; ++i) {                       // one round more than choices: the distance to the next best
@@ -254,12 +284,14 @@ __device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC
                 for (int j = 0; j < 4; ++j) m[r] = larger(m[r], key[r][c][j]);
         }
         row_max(m);
+        if constexpr (ASK)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const T v = O::value(m[r]);
-            close |= last[r] - v <= tol ? 1 : 0;
-            last[r] = v;
-        }
+            for (int r = 0; r < R; ++r) {
+                const float v = O::value(m[r]);
+                close |= last[r] - v <= reach[r] ? 1 : 0;   // (from none to none: NaN, not close)
+                last[r] = v;
+                reach[r] = 2.f * fmaf(err.rel, fabsf(v), err.base);
+            }
         int at[R], e[R];                                   // the lane's first expert with that key; the row's first loses it
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -374,17 +406,17 @@ __device__ __forceinline__ void select_exact(const smoe_topk_args& a, int tok, t
 #pragma unroll
         for (int j = 0; j < 4; ++j) key[0][c][j] = served && sl[c][j] < 0 ? -INFINITY : key[0][c][j];
     int mine[1];
-    keep_groups<double, EC>(key[0], a, sub, 0.0);
-    pick_row<double, EC, 1>(key, a, sub, 0.0, mine);
+    keep_groups<double, EC>(key[0], a, sub, key_error{});
+    pick_row<double, EC, 1>(key, a, sub, key_error{}, mine);
     store_choice<double>(a, mine[0], [&](int e) { return s.score[e] * inv_z; }, [&](int e) { return s.logit[e]; }, sub, tok, served,
                          served ? a.slot : a.orig_expert, served ? a.gate : a.orig_gate, lane < 32);
 }
 
-// Whether another lane of the row holds a value within tol.
+// Whether another lane of the row holds a value that may be equal, each being off by at most `off`.
 template <int N = 1>
-__device__ __forceinline__ bool near_in_row(float v, float tol) {
-    bool near = fabsf(v - dpp<0x120 + N>(v)) <= tol;
-    if constexpr (N < 15) near |= near_in_row<N + 1>(v, tol);
+__device__ __forceinline__ bool near_in_row(float v, float off) {
+    bool near = fabsf(v - dpp<0x120 + N>(v)) <= off + dpp<0x120 + N>(off);
+    if constexpr (N < 15) near |= near_in_row<N + 1>(v, off);
     return near;
 }
 
@@ -393,7 +425,6 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
     const int lane = threadIdx.x & 63, per = a.E / a.groups;
     float* fkey = (float*)s.score;
     float* rkey = fkey + 64 * EC;
-    float most = 0.f;
 #pragma unroll 1
     for (int e = lane; e < 64 * EC; e += 64) {
         const float l = e < a.E ? logit_at(e) : -INFINITY;
@@ -401,10 +432,8 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
         s.logit[e] = l;
         fkey[e] = key;
         rkey[e] = e < a.E && a.e2s[e] >= 0 ? key : -INFINITY;
-        most = fmaxf(most, e < a.E ? fabsf(key) : 0.f);
     }
-    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-    const float tol = 2.f * (a.by_logit ? err : 0.25f * err + 4.8e-7f * (most + 1.f));
+    const key_error off = {a.by_logit ? err : 0.25f * err + 8 * HALF_STEP, a.by_logit ? 0.f : HALF_STEP};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // lanes of a wave read what others wrote: its LDS accesses are in order
     // Groups whose rank is near another's, and the least key of those that make a group's rank (lane g: group g).
     bool near_group[2] = {false, false};
@@ -427,16 +456,17 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
                 }
             }
             made_of[res] = a.best == 2 ? m2 : m1;
-            const float rank = a.best == 2 && m2 > -INFINITY ? m1 + m2 : m1;
-            near_group[res] = near_in_row(rank, 2.f * tol);    // (lanes behind the groups are infinitely far)
+            const float rank = a.best == 2 && m2 > -INFINITY ? fmaxf(m1 + m2, -FLT_MAX) : m1;
+            near_group[res] = near_in_row(rank, rank_error(a, m1, m2, rank, off));   // (lanes behind the groups are infinitely far)
         }
     }
     unsigned again_of = 0;                                 // bit c: this lane's expert of chunk c
-    float mine[EC];
+    float mine[EC], tol[EC];
     int near[EC];
 #pragma unroll
     for (int c = 0; c < EC; ++c) {
         mine[c] = fkey[64 * c + lane];
+        tol[c] = mine[c] > -INFINITY ? 2.f * fmaf(off.rel, fabsf(mine[c]), off.base) : 0.f;
         near[c] = 0;
     }
 #pragma unroll 1
@@ -446,7 +476,7 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int c = 0; c < EC; ++c) near[c] += fabsf(mine[c] - o[i]) <= tol;
+            for (int c = 0; c < EC; ++c) near[c] += fabsf(mine[c] - o[i]) <= tol[c];
     }
 #pragma unroll
     for (int c = 0; c < EC; ++c) {
@@ -457,7 +487,7 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
             const float least = __shfl(made_of[0], g), least_res = __shfl(made_of[1], g);
             again |= (in_all && mine[c] >= least) || (in_res && rkey[e] == mine[c] && mine[c] >= least_res);
         }
-        again_of |= (again && e < a.E ? 1u : 0u) << c;
+        again_of |= (again && e < a.E && mine[c] > -INFINITY ? 1u : 0u) << c;   // (what cannot be had is not asked for)
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     int* list = (int*)fkey;                                // the keys have been used up
@@ -648,9 +678,9 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             const float l = logit_at(e);
             return a.sigmoid ? sigmoid_of(l) : expf(l - top) * inv_z;
         };
-        float tol = err;
+        key_error off = {err, 0.f};
         if (!a.by_logit) {
-            float most = 0.f;
+            float most = 0.f;                              // largest score
 #pragma unroll
             for (int c = 0; c < EC; ++c)
 #pragma unroll
@@ -658,13 +688,14 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
                     const bool in = 64 * c + 4 * sub + j < a.E;
                     const float s = a.sigmoid ? sigmoid_near(v[c][j]) : expf(v[c][j] - top) * inv_z;
                     v[c][j] = in ? s + bias[c][j] : -INFINITY;
-                    most = fmaxf(most, in ? fmaxf(fabsf(v[c][j]), s) : 0.f);
+                    most = fmaxf(most, in ? s : 0.f);
                 }
             // a sigmoid is off by at most a quarter of its logit's error, a share of a softmax by at most twice its own size times that; and the
-            // exponential, the quotient and the sum with the bias are rounded: units of 2^-24, 8 of them, and of the fast sigmoid s another
-            // 1.5 (1 - s) |l|, where s (1 - s) |l| <= (|largest l| + 1/2) (largest s)
+            // exponential and the quotient are rounded: units of 2^-24, 8 of them, and of the fast sigmoid s another
+            // 1.5 (1 - s) |l|, where s (1 - s) |l| <= (|largest l| + 1/2) (largest s); and the sum with the bias, half a step of its own
             const float units = a.sigmoid ? 8.f + 2.f * fabsf(top) : 8.f;
-            tol = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + 0x1p-24f * units * __int_as_float(row_max(__float_as_int(most)));
+            off.base = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + HALF_STEP * units * __int_as_float(row_max(__float_as_int(most)));
+            off.rel = HALF_STEP;
         }
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -682,9 +713,9 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
                 for (int c = 0; c < EC; ++c)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) key[r][c][j] = to_ordered(first + r && sl[c][j] < 0 ? -INFINITY : v[c][j]);
-                if (a.groups > 1) close |= keep_groups<float, EC>(key[r], a, sub, 2.f * tol);
+                if (a.groups > 1) close |= keep_groups<float, EC>(key[r], a, sub, off);
             }
-            close |= pick_row<float, EC, R>(key, a, sub, 2.f * tol, mine);
+            close |= pick_row<float, EC, R>(key, a, sub, off, mine);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const bool served = first + r;
