@@ -132,12 +132,13 @@ __device__ __forceinline__ int group_of(const smoe_topk_args& a, int e) { return
 // counts where its own key is compared and nowhere else.
 struct key_error {
     float base, rel;
+    float left_out;                                        // of every key: what a group of two has more of than a single expert
 };
 constexpr float HALF_STEP = 0x1p-24f;
 
 // How far the rank of a group may be off, from its largest keys (best = 1: the first alone); 0 where the group has none.
 __device__ __forceinline__ float rank_error(const smoe_topk_args& a, float m1, float m2, float rank, key_error err) {
-    const float one = err.base + err.rel * fabsf(m1), two = one + err.base + err.rel * fabsf(m2) + HALF_STEP * fabsf(rank);
+    const float one = err.base + err.rel * fabsf(m1), two = one + err.base + err.rel * fabsf(m2) + (m1 + m2 != 0.f ? HALF_STEP * fabsf(rank) : 0.f);
     return rank == -INFINITY ? 0.f : a.best == 2 && m2 > -INFINITY ? two : one;
 }
 
@@ -170,7 +171,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             if (lanes >= 4) merge(dpp<0x4E>(m1), dpp<0x4E>(m2));
             if (lanes >= 8) merge(dpp<0x141>(m1), dpp<0x141>(m2));   // the other quad of eight lanes
             if (lanes >= 16) merge(dpp<0x140>(m1), dpp<0x140>(m2));  // the other eight
-            rank[c] = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
+            rank[c] = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2) + T(err.left_out), last_key(T(0)))) : m1;
             if constexpr (ASK) off[c] = rank_error(a, O::value(m1), O::value(m2), O::value(rank[c]), err);
         }
         int ahead[EC];
@@ -201,10 +202,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
 #pragma unroll
             for (int j = 0; j < 4; ++j) key[c][j] = keep ? key[c][j] : none;
         }
-        if constexpr (ASK) {
-            next = row_max(next);
-            close = row_min(worst) <= next && next > -INFINITY ? 2 : 0;
-        }
+        if constexpr (ASK) close = row_min(worst) < row_max(next) ? 2 : 0;
     } else if (a.groups > 1) {
         I rank = none;                                     // of group `sub`
         float off = 0.f;
@@ -231,7 +229,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
             merge(dpp<0x124>(m1), dpp<0x124>(m2));
             merge(dpp<0x122>(m1), dpp<0x122>(m2));
             merge(dpp<0x121>(m1), dpp<0x121>(m2));
-            const I r = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2), last_key(T(0)))) : m1;
+            const I r = a.best == 2 && m2 > none ? O::of(larger(O::value(m1) + O::value(m2) + T(err.left_out), last_key(T(0)))) : m1;
             rank = g == sub ? r : rank;
             if constexpr (ASK) off = g == sub ? rank_error(a, O::value(m1), O::value(m2), O::value(r), err) : off;
         }
@@ -245,8 +243,7 @@ __device__ __forceinline__ int keep_groups(typename key_order<T>::type (&key)[EC
         }
         if constexpr (ASK) {
             const bool mine = kept >> sub & 1u;
-            const float worst = row_min(mine ? O::value(rank) - off : INFINITY), next = row_max(mine ? -INFINITY : O::value(rank) + off);
-            close = worst <= next && next > -INFINITY ? 2 : 0;
+            close = row_min(mine ? O::value(rank) - off : INFINITY) < row_max(mine ? -INFINITY : O::value(rank) + off) ? 2 : 0;
         }
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -270,7 +267,7 @@ __device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC
     for (int r = 0; r < R; ++r) {
         mine[r] = -1;
         last[r] = INFINITY;
-        reach[r] = -1.f;                                   // the first is near nothing
+        reach[r] = 0.f;
     }
 #pragma unroll 1
     for (int i = 0; i <= a.k; ++i) {                       // one round more than choices: the distance to the next best
@@ -288,7 +285,7 @@ __device__ __forceinline__ int pick_row(typename key_order<T>::type (&key)[R][EC
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float v = O::value(m[r]);
-                close |= last[r] - v <= reach[r] ? 1 : 0;   // (from none to none: NaN, not close)
+                close |= last[r] - v < reach[r] ? 1 : 0;   // (keys without errors: equal ones are a tie; from none to none: NaN)
                 last[r] = v;
                 reach[r] = 2.f * fmaf(err.rel, fabsf(v), err.base);
             }
@@ -433,7 +430,7 @@ __device__ __forceinline__ void choose_exact(const smoe_topk_args& a, int tok, A
         fkey[e] = key;
         rkey[e] = e < a.E && a.e2s[e] >= 0 ? key : -INFINITY;
     }
-    const key_error off = {a.by_logit ? err : 0.25f * err + 8 * HALF_STEP, a.by_logit ? 0.f : HALF_STEP};
+    const key_error off = {a.by_logit ? err : 0.25f * err + 8 * HALF_STEP, a.by_logit ? 0.f : HALF_STEP, 0.f};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); // lanes of a wave read what others wrote: its LDS accesses are in order
     // Groups whose rank is near another's, and the least key of those that make a group's rank (lane g: group g).
     bool near_group[2] = {false, false};
@@ -554,6 +551,18 @@ __device__ __forceinline__ float4 load_x4(const smoe_topk_args& a, size_t at) {
     return make_float4(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xFFFF0000u));
 }
 
+// Whether token tok's row of x is all zeros, by its 16 lanes.
+__device__ __forceinline__ bool zero_row(const smoe_topk_args& a, int tok, int sub) {
+    const uint4* row = (const uint4*)((const char*)a.x + (size_t)tok * a.d * (a.f32 ? 4 : 2));
+    const uint32_t bits = a.f32 ? 0x7fffffffu : 0x7fff7fffu;   // -0 is a zero
+    uint32_t any = 0;
+    for (int c = sub; c < (a.f32 ? a.d >> 2 : a.d >> 3); c += 16) {
+        const uint4 v = row[c];
+        any |= (v.x | v.y | v.z | v.w) & bits;
+    }
+    return row_max(any ? 1 : 0) == 0;
+}
+
 // Where a bias meets the softmax every key holds the sum over all experts, and all logits are computed again: lane l's are those of the experts
 // 64 c + l, over the columns 4 q0 .. 4 q1 - 1.
 template <int EC>
@@ -652,7 +661,21 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
 #pragma unroll
         for (int q = 0; q < 2 * NS; ++q) ss += sqp[t + q * NTOK];
         const float xnorm = sqrtf(ss);
-        const float err = 0x1p-24f * (a.err_norm * xnorm * wnorm + a.err_sum * __int_as_float(row_max(__float_as_int(big))));
+        big = __int_as_float(row_max(__float_as_int(big)));
+        float err = HALF_STEP * (a.err_norm * xnorm * wnorm + a.err_sum * big);
+        // A row of zeros, as padding has them: its logits are zeros and its scores equal, both exactly, so its keys are the biases, without an error.  (16384
+        // tokens, half of them zeros, 8 of 128 experts in groups: 51 us; with all their choices counted as close, and repeated in 64 bits, 1210.)
+        const bool faint = ss < 0x1p-100f;
+        bool zeros = false;
+        if (__any(faint)) {
+            int numbers = 1;
+#pragma unroll
+            for (int c = 0; c < EC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) numbers &= v[c][j] == v[c][j];
+            zeros = zero_row(a, min(tok, a.T - 1), sub) && row_min(numbers);
+            if (faint && !zeros) err = INFINITY;           // squares that underflow say nothing about the error: all in 64 bits
+        }
         float top = -INFINITY, z = 1.f;
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -678,7 +701,7 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             const float l = logit_at(e);
             return a.sigmoid ? sigmoid_of(l) : expf(l - top) * inv_z;
         };
-        key_error off = {err, 0.f};
+        key_error off = {err, 0.f, 0.f};
         if (!a.by_logit) {
             float most = 0.f;                              // largest score
 #pragma unroll
@@ -696,6 +719,13 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             const float units = a.sigmoid ? 8.f + 2.f * fabsf(top) : 8.f;
             off.base = (a.sigmoid ? 0.25f : 2.f * inv_z) * err + HALF_STEP * units * __int_as_float(row_max(__float_as_int(most)));
             off.rel = HALF_STEP;
+        }
+        if (zeros) {
+            off = {0.f, HALF_STEP, a.sigmoid ? 0.5f : inv_z};   // (the second for sums of two)
+#pragma unroll
+            for (int c = 0; c < EC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[c][j] = 64 * c + 4 * sub + j < a.E ? bias[c][j] : -INFINITY;
         }
 #pragma unroll
         for (int c = 0; c < EC; ++c)
@@ -715,7 +745,7 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
                     for (int j = 0; j < 4; ++j) key[r][c][j] = to_ordered(first + r && sl[c][j] < 0 ? -INFINITY : v[c][j]);
                 if (a.groups > 1) close |= keep_groups<float, EC>(key[r], a, sub, off);
             }
-            close |= pick_row<float, EC, R>(key, a, sub, off, mine);
+            close |= pick_row<float, EC, R>(key, a, sub, zeros ? key_error{} : off, mine);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const bool served = first + r;
