@@ -511,8 +511,12 @@ class Layer:
     def block_topk(self, x, T, weight, eps, rule, y, residual=None, total=None, bias=None, accumulate=1, out=None, q=None,
                    q_scale=None):
         """A whole pre-norm block: total = x + residual, y = norm(total) (in 8 bits too where q is given), the layer on y,
-        and total added to its result.  total None: x itself is the stream (then residual must be None)."""
+        and total added to its result.  total None: x itself is the stream (then residual must be None).  y may lie over x or
+        residual, but not over the stream, which is still needed; out may lie over any of them."""
         if total is None and residual is not None:
             raise ValueError("block_topk: the sum of x and residual needs a buffer (total)")
+        stream = x if total is None else total
+        if y is not None and _ptr(y) == _ptr(stream):
+            raise ValueError("block_topk: y lies over the stream, which is added to the layer's result")
         self.add_norm(x, T, weight, eps, residual, total, y, q, q_scale)
-        return self.forward_topk(y, T, rule, bias, accumulate, x if total is None else total, out, q, q_scale)
+        return self.forward_topk(y, T, rule, bias, accumulate, stream, out, q, q_scale)
