@@ -497,6 +497,8 @@ class Layer:
     def forward_topk(self, x, T, rule, bias=None, accumulate=1, residual=None, out=None, q=None, q_scale=None):
         """Route, importance, sort, expert FFN and weighted sum with rule.k experts per token.  Layers with 8-bit slots
         take the rows of x in 8 bits too (q, q_scale of add_norm)."""
+        if self.dtype == SMOE_MXFP8 and (q is None or q_scale is None):
+            raise ValueError("forward_topk: a layer with 8-bit slots needs the rows in 8 bits too (q, q_scale)")
         k = rule.k
         self.route_topk(x, T, rule, bias)
         self.importance(T * k, accumulate)
@@ -518,5 +520,7 @@ class Layer:
         stream = x if total is None else total
         if y is not None and _ptr(y) == _ptr(stream):
             raise ValueError("block_topk: y lies over the stream, which is added to the layer's result")
+        if self.dtype == SMOE_MXFP8 and (q is None or q_scale is None):
+            raise ValueError("block_topk: a layer with 8-bit slots needs buffers for the rows in 8 bits (q, q_scale)")
         self.add_norm(x, T, weight, eps, residual, total, y, q, q_scale)
         return self.forward_topk(y, T, rule, bias, accumulate, stream, out, q, q_scale)

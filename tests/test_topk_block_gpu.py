@@ -36,3 +36,18 @@ def test_the_norm_may_not_lie_over_the_stream(dtype):
         torch.cuda.synchronize()
         assert torch.equal(got, want), over
     L.close()
+
+
+def test_8_bit_layers_need_the_rows_in_8_bits():
+    T, k = 12, 2
+    L, w1, w2, router, resident, x, r, nw, act = _pass_case(b.SMOE_MXFP8, T, k)
+    L.count.fill_(5)
+    q, qs = L.mx_buffers(T)
+    for kw in (dict(), dict(q=q), dict(q_scale=qs)):
+        with pytest.raises(ValueError):
+            L.forward_topk(x, T, b.smoe_topk_rule(k), **kw)
+        with pytest.raises(ValueError):
+            L.block_topk(x, T, nw, EPS, b.smoe_topk_rule(k), torch.empty_like(x), **kw)
+    torch.cuda.synchronize()
+    assert (L.count == 5).all()                            # nothing has been counted
+    L.close()
