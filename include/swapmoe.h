@@ -369,8 +369,9 @@ typedef struct {
  *       slot -1, gate 0 (softmax still runs over all E, renorm over the served)
  *   xnorm [T, k]                   |x_t|, k times
  * so that smoe_importance takes the T * k pairs as they are.  The layer's
- * gate_mode plays no part.  Choices nearer to one another than the error of an
- * fp32 logit are decided again in 64 bits.  The first call after a bind
+ * gate_mode plays no part.  Choices nearer to one another than an estimate of the
+ * error of their fp32 logits are decided again in 64 bits; the estimate is above the
+ * errors measured on many kinds of rows, but no bound.  The first call after a bind
  * prepares the router's weights in the workspace; router_w must still hold them at
  * later calls.  A token with a NaN takes experts like any other, those whose logits are NaN
  * behind the others in the order of their ids, and their weights are NaN.

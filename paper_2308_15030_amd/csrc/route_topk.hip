@@ -13,8 +13,10 @@
 // Without a bias, and with single experts ranking the groups, the keys are the logits themselves, of which every score is a rising
 // function.
 
+#include <algorithm>
 #include <cfloat>
 #include <climits>
+#include <cmath>
 #include <type_traits>
 
 #include "route_mfma.h"
@@ -967,12 +969,15 @@ int smoe_launch_route_topk(const smoe_layer* L, const smoe_topk_rule& rule, cons
     a.inv_per = 1.f / per;
     a.aligned = per >= 4 && per <= 64 && !(per & (per - 1));
     // The partial sums of a logit pass through n roundings.  Where x points nowhere in particular they are small, and the error measured at
-    // most 0.75 |x| |w| 2^-24 (bf16; fp32: 1.3) in batches of 16384 tokens, 64 .. 16384 columns and up to 256 experts.  Where x follows a row of the
-    // router they grow to the logit's own size (seen in the slices' sums also where these cancel), and it measured 0.08 n of it.
+    // most 1.0 |x| |w| 2^-24 (256 .. 16384 columns, up to 256 experts).  Where x follows a row of the router they grow to the logit's own size (seen in the
+    // slices' sums also where these cancel), and it measured up to 1.8 + 0.08 n of it.  Where x follows a row for half of a slice and its negative for the other
+    // half, they grow and vanish inside the slice, unseen: 2.3, 3.6 and 9.8 |x| |w| 2^-24 at 1024, 4096 and 16384 columns in bf16 (n = 48, 192, 768), 3.5, 5.6 and
+    // 13.6 in fp32 (128, 512, 2048), at most 0.36 sqrt(n).  All kinds of rows measured at most 0.84 of the sum of both terms; it is an
+    // estimate, not a bound, which would be n |x| |w| 2^-24.
     const int slices = c.E <= 32 ? 8 : 4;
     const int n = a.f32 ? 4 * (((c.d_model + 7) / 8 + slices - 1) / slices) : 3 * ((c.d_model / 16 + slices - 1) / slices);
-    a.err_norm = a.f32 ? 1.5f : 1.f;
-    a.err_sum = 1.f + 0.1f * n;
+    a.err_norm = std::max(1.f, 0.36f * std::sqrt((float)n));
+    a.err_sum = 2.f + 0.1f * n;
     if (topk_few(c, T)) {
         a.logits = (double*)L->d_hidden;                   // scratch that the products after it fill
         hipLaunchKernelGGL(topk_logits_kernel, dim3((c.E + 3) / 4, (T + FEW_TOK - 1) / FEW_TOK), dim3(256), 0, s, a);
