@@ -236,9 +236,9 @@ int smoe_bind(smoe_layer_t* L, const float* router_w, void* slot_w1, void* slot_
     L->d_hidden = L->workspace + w.hidden;
     L->d_router_split = L->workspace + w.rsplit;
     L->d_route_part = L->workspace + w.rpart;
-    L->router_split_done = false;
+    L->router_split = smoe_once_state{};
     L->d_router_norm = (float*)(L->workspace + w.rnorm);
-    L->router_topk_done = false;
+    L->router_norm = smoe_once_state{};
     L->ws_ready = false;
     L->d_norm_partial = (float*)(L->workspace + w.norm);
     std::fill(L->slot_to_expert.begin(), L->slot_to_expert.end(), -1);
@@ -566,6 +566,11 @@ int smoe_check_hot(const smoe_layer* L, int T, const char* who, bool need_full) 
 
 void smoe_note_slot_pass(smoe_layer* L) { note_slot_pass(L); }
 
+int smoe_prepare_router(smoe_layer* L, const char* who, hipStream_t s) {
+    if (L->cfg.dtype == SMOE_F32) return SMOE_OK;
+    return smoe_once(L->router_split, who, s, [&] { return smoe_launch_split_router(L, s); });
+}
+
 extern "C" {
 
 int smoe_route(smoe_layer_t* L, const void* x, int T, int32_t* orig_expert, float* orig_gate,
@@ -576,11 +581,7 @@ int smoe_route(smoe_layer_t* L, const void* x, int T, int32_t* orig_expert, floa
     if (!x || !orig_expert || !orig_gate || !slot || !gate || !xnorm)
         return smoe_fail(SMOE_EINVAL, "smoe_route: null buffer");
     if (misaligned(x, 16)) return smoe_fail(SMOE_EINVAL, "smoe_route: x must be 16-byte aligned");
-    if (L->cfg.dtype != SMOE_F32 && !L->router_split_done) {
-        rc = smoe_launch_split_router(L, as_stream(stream));
-        if (rc) return rc;
-        L->router_split_done = true;
-    }
+    if ((rc = smoe_prepare_router(L, "smoe_route", as_stream(stream)))) return rc;
     return smoe_launch_route(L, x, T, orig_expert, orig_gate, slot, gate, xnorm, nullptr, as_stream(stream));
 }
 
@@ -674,11 +675,7 @@ int smoe_forward(smoe_layer_t* L, const void* x, int T, const void* residual, vo
     if (x == out) return smoe_fail(SMOE_EINVAL, "smoe_forward: out must not alias x");
     hipStream_t s = as_stream(stream);
     struct Noted { smoe_layer* L; ~Noted() { note_slot_pass(L); } } noted{L};   // after the launches, which ask what came before
-    if (!L->router_split_done) {
-        rc = smoe_launch_split_router(L, s);
-        if (rc) return rc;
-        L->router_split_done = true;
-    }
+    if ((rc = smoe_prepare_router(L, "smoe_forward", s))) return rc;
     if (smoe_decode_first_applies(L, T) && smoe_ffn_dense_path(L, T)) {
         // the router next to the first product of every slot (or in front of the first product of the slots
         // that got tokens), then the second product of those slots next to ranking and importance

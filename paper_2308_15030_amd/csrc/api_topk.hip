@@ -61,16 +61,8 @@ int smoe_route_topk(smoe_layer_t* L, const smoe_topk_rule* rule, const float* bi
     if (smoe_misaligned(x, 16)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: x must be 16-byte aligned");
     if (smoe_misaligned(bias, 4)) return smoe_fail(SMOE_EINVAL, "smoe_route_topk: bias must be 4-byte aligned");
     const hipStream_t s = (hipStream_t)stream;
-    if (!L->router_topk_done) {
-        // a capture only records the preparation: the next call outside of it still has to run its own, also where a smoe_route in a
-        // capture has recorded the router's weights already
-        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-        if (int rc = smoe_check_hip(hipStreamIsCapturing(s, &capture), "smoe_route_topk: capture status")) return rc;
-        if (c.dtype != SMOE_F32)
-            if (int rc = smoe_launch_split_router(L, s)) return rc;
-        if (int rc = smoe_launch_router_norm(L, s)) return rc;
-        if (capture == hipStreamCaptureStatusNone) L->router_split_done = L->router_topk_done = true;
-    }
+    if (int rc = smoe_prepare_router(L, "smoe_route_topk", s)) return rc;
+    if (int rc = smoe_once(L->router_norm, "smoe_route_topk", s, [&] { return smoe_launch_router_norm(L, s); })) return rc;
     return smoe_launch_route_topk(L, r, bias, x, T, orig_expert, orig_gate, slot, gate, xnorm, s);
 }
 

@@ -31,6 +31,12 @@ struct smoe_step_tail {
     int32_t* offsets;
 };
 
+// Work that a bind leaves to the first call (smoe_once).
+struct smoe_once_state {
+    bool done = false;
+    unsigned long long capture = ~0ull;      // the capture that has recorded it last
+};
+
 struct smoe_layer {
     smoe_config cfg;
     mutable smoe_step_tail tail{};           // left by a small batch's first launch for its second
@@ -83,9 +89,8 @@ struct smoe_layer {
     bool load_from_host = false;             // set around a load's launch: its source is pinned host memory
     void* d_router_split = nullptr;          // bf16 path: router weights in matrix-operand order
     void* d_route_part = nullptr;            // small batches: partial logits and sums of squares of at most SMOE_FEW_T tokens
-    bool router_split_done = false;          // made by the first smoe_route after a bind
     float* d_router_norm = nullptr;          // largest |w_e| of the router's rows (smoe_route_topk)
-    bool router_topk_done = false;           // it and d_router_split, made by the first smoe_route_topk after a bind
+    smoe_once_state router_split, router_norm;   // d_router_split and d_router_norm are made by the first calls after a bind
 
     hipEvent_t prof_ev[4] = {nullptr, nullptr, nullptr, nullptr};   // one-shot FFN profiling events
     hipEvent_t bracket[2] = {nullptr, nullptr};                     // smoe_profile_begin / _end
@@ -109,6 +114,22 @@ int smoe_check_hip(hipError_t e, const char* what);
 // What the calls on a batch have in common: a bound handle, 0 <= T <= max_tokens and, with need_full, every slot filled.
 int smoe_check_hot(const smoe_layer* L, int T, const char* who, bool need_full);
 void smoe_note_slot_pass(smoe_layer* L);
+// Runs `launch` unless it has run: a capture only records it, once, and what runs outside of that capture needs its own.
+template <class F>
+inline int smoe_once(smoe_once_state& st, const char* who, hipStream_t s, F launch) {
+    if (st.done) return SMOE_OK;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (int rc = smoe_check_hip(hipStreamGetCaptureInfo(s, &status, &id), who)) return rc;
+    const bool capture = status != hipStreamCaptureStatusNone;
+    if (capture && st.capture == id) return SMOE_OK;
+    if (int rc = launch()) return rc;
+    if (capture) st.capture = id;
+    else st.done = true;
+    return SMOE_OK;
+}
+// The router's weights in operand order, for layers of bf16 activations.
+int smoe_prepare_router(smoe_layer* L, const char* who, hipStream_t s);
 inline bool smoe_misaligned(const void* p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
 // Activations and the experts of the bank: fp32, or bf16 for every other type of layer.
