@@ -30,7 +30,8 @@
  *   - Calls on one handle must be issued from one thread at a time, and stream
  *     work of consecutive calls on one handle must be ordered (same stream, or
  *     event dependencies), because they share the bound workspace.
- *   - NaN / Inf inputs give undefined results.
+ *   - NaN / Inf inputs give undefined results, except where a call says what
+ *     they give.
  */
 #ifndef SWAPMOE_H
 #define SWAPMOE_H
@@ -331,8 +332,8 @@ size_t smoe_mx_scale_pitch(int d_model);
 /* Residual addition and root-mean-square norm, for each of T rows:
  *   h = x + residual (residual may be NULL);  total = h
  *   y = h / sqrt(mean(h^2) + eps) * weight;  q, q_scale = y as 8-bit rows
- * computed in fp32 from the unrounded sum; total and y are rounded once to the
- * layer's activation type.  weight [d_model] fp32, 16-byte aligned.  Any of
+ * computed in fp32 from the unrounded sum (so sum h^2 has to lie in its range); total
+ * and y are rounded once to the layer's activation type.  weight [d_model] fp32, 16-byte aligned.  Any of
  * total, y and the pair (q, q_scale) may be NULL, not all; 8-bit rows need
  * d_model % 32 == 0, and their bytes behind the last block of a row of q_scale
  * become 0.  total and y may alias x or residual, but not each other.  Uses the
@@ -397,7 +398,8 @@ int smoe_permute_topk(smoe_layer_t* layer, const void* x, const int32_t* slot, i
  * slot's matrices, which smoe_set_resident and smoe_update_tick round from the bf16
  * bank to blocks of 32 consecutive elements of a column (along the reduction), and h rounded
  * to blocks of 32 features between the products; products and sums on the
- * matrix cores in fp32, y_perm bf16, rounded once.  Rows from offsets[K] on are
+ * matrix cores, which add 8 products at a time to 2^-13 of the largest of them and
+ * those sums in fp32, y_perm bf16, rounded once.  Rows from offsets[K] on are
  * left as they were.  A row with a NaN among its values becomes NaN throughout;
  * other rows' bits do not depend on it. */
 int smoe_expert_ffn_mx(smoe_layer_t* layer, const void* q, const void* q_scale, const int32_t* perm, int k,

@@ -358,8 +358,8 @@ __global__ __launch_bounds__(256, FB == 8 ? 2 : 3) void tile_mx_kernel(const MxA
     }
     const int sblk = FB == 8 ? 2 * wave + ((lane >> 4) & 1) : wave % FB;      // scales: 16 lanes a block
     const char* wscale = wslot + (size_t)nfb * rowb + (size_t)(fb0 + min(sblk, width - 1)) * rows_ + (lane & 15) * 16;
-    const int unit = (lane & 3) ^ ((lane >> 3) & 3);       // rows of 64 bytes whose four units are permuted by (row / 2) % 4: operand reads of
-                                                           // neighbouring lanes hit all banks
+    const int unit = (lane & 3) ^ ((lane >> 3) & 3);       // rows of 64 bytes whose four units are permuted by (row / 2) % 4: of 16 lanes that read
+                                                           // operands, two meet in each group of banks (4 cycles a read of the first product)
     const char *tsrc[2], *tscale = nullptr;                // FIRST: this lane's two rows of block `wave`; else a scalar base (tsrc[0])
     const uint64_t tlanes = wave < nb ? ~0ull : 1;
     const int bc = min(wave, nb - 1);

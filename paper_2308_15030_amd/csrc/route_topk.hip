@@ -936,9 +936,9 @@ __global__ __launch_bounds__(1024) void router_norm_kernel(const float* __restri
 
 // Whether T tokens take the launches for few tokens: where one workgroup's walk through the router takes longer than a second launch.  bf16 from
 // 256 KB of router on, fp32 always (its matrix products are slow).  Measured with 2 choices (us, one launch / two): bf16, 64 experts of 768 columns,
-// 1 token 7.7 / 7.9, 128 tokens 8.8 / 9.4; 64 of 1024 8.8 / 8.5 and 9.9 / 10.1; 128 of 512 9.9 / 8.5 and 11.1 / 10.5; 128 of 1024 13.1 / 9.7 and
-// 14.6 / 12.7 (256 tokens: 15.3 / 16.9); 256 of 2048 39 / 15 and 41 / 26; fp32, 64 of 768 13.7 / 7.3 and 17.2 / 8.4, 512 tokens
-// 17.4 / 12.5, 1024 17.4 / 17.4; 16 of 512 at 512 tokens 9.8 / 8.2, 128 of 1024 31 / 20, at 1024 31 / 33.
+// 1 token 8.9 / 9.0, 128 tokens 9.9 / 10.3; 64 of 1024 10.1 / 9.4 and 11.1 / 11.0; 128 of 512 11.4 / 9.6 and 12.5 / 11.6; 128 of 1024 14.7 / 10.9 and
+// 15.9 / 13.7 (256 tokens: 16.0 / 17.4); 256 of 2048 40 / 16 and 42 / 28; fp32, 64 of 768 14.7 / 8.3 and 18.2 / 9.4, 512 tokens
+// 18.5 / 13.3, 1024 18.5 / 18.2; 16 of 512 at 512 tokens 10.6 / 9.1, 128 of 1024 32 / 22, at 1024 32 to 39 / 35.
 bool topk_few(const smoe_config& c, int T) { return T <= smoe_topk_few_tokens(c.dtype) && (c.dtype == SMOE_F32 || c.E * c.d_model >= 65536); }
 
 }  // namespace
