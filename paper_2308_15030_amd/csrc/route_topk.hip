@@ -723,11 +723,11 @@ __device__ __forceinline__ void smoe_route_finish(const int block, const smoe_to
             off.rel = HALF_STEP;
         }
         if (zeros) {
-            off = {0.f, HALF_STEP, a.sigmoid ? 0.5f : inv_z};   // (the second for sums of two)
+            off = {0.f, a.best == 2 ? HALF_STEP : 0.f, a.sigmoid ? 0.5f : inv_z};   // (the second for sums of two)
 #pragma unroll
             for (int c = 0; c < EC; ++c)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[c][j] = 64 * c + 4 * sub + j < a.E ? bias[c][j] : -INFINITY;
+                for (int j = 0; j < 4; ++j) v[c][j] = 64 * c + 4 * sub + j < a.E ? bias[c][j] + 0.f : -INFINITY;   // (-0 is no less than 0)
         }
 #pragma unroll
         for (int c = 0; c < EC; ++c)

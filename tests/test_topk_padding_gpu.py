@@ -11,7 +11,8 @@ from test_topk_masks_gpu import time_us
 
 pytestmark = pytest.mark.gpu
 RULES = [("softmax", 1, 1, 1, None), ("sigmoid", 1, 1, 1, None), ("sigmoid", 4, 2, 2, None), ("softmax", 4, 2, 2, None), ("sigmoid", 8, 3, 2, "some"),
-         ("softmax", 8, 3, 2, "some"), ("sigmoid", 1, 1, 1, "some"), ("softmax", 1, 1, 1, "zero"), ("sigmoid", 4, 3, 2, "zero"), ("sigmoid", 1, 1, 1, "inf")]
+         ("softmax", 8, 3, 2, "some"), ("sigmoid", 1, 1, 1, "some"), ("softmax", 1, 1, 1, "zero"), ("sigmoid", 4, 3, 2, "zero"), ("sigmoid", 1, 1, 1, "signed"), ("softmax", 4, 2, 2, "signed"), ("sigmoid", 4, 2, 1, "steps"),
+         ("sigmoid", 4, 2, 2, "steps"), ("sigmoid", 1, 1, 1, "inf")]
 
 
 def _bias(how, E, g):
@@ -20,6 +21,10 @@ def _bias(how, E, g):
     v = 0.1 * torch.randn(E, generator=g) if how != "zero" else torch.zeros(E)
     if how == "inf":
         v[::3] = -np.inf
+    if how == "signed":                                    # zeros of either sign, which are equal
+        v = torch.where(torch.rand(E, generator=g) < 0.5, -0.0, 0.0)
+    if how == "steps":                                     # many equal ones
+        v = 0.125 * torch.randint(-1, 2, (E,), generator=g)
     return v.to(DEV)
 
 
